@@ -31,6 +31,7 @@
  *    quantized); unpacked int8 codes support any b in [2,8].
  *  - `status` (nullable) is a device uint32 that is OR-ed into, never cleared:
  *    bit 0 = a scale delta was not finite (NaN/Inf in the input vector);
+ *    bit 1 = a class (label, teacher's entry) was not below the number of classes;
  *    bit 31 = dq_run_rounds, where the blocks of one launch do many rounds: they waited for each other
  *    for seconds and gave up, the state is not that of the rounds asked for.  (Without a status word no launch does
  *    many rounds that way.)
@@ -310,6 +311,101 @@ int32_t dq_acc_params(float lr, int64_t s, float *theta_out /*host*/, float *eta
 int32_t dq_acc_mix(const float *y, const float *x_snap, float theta, int64_t d, float *x_out, void *stream);
 /* End of an epoch of Alg. 3:  x_snap_out = xsum / m. */
 int32_t dq_acc_snapshot(const float *xsum, int64_t m, int64_t d, float *x_snap_out, void *stream);
+
+/* ---- models of many classes ------------------------------------------------------- */
+
+/* The binary model of eq. (1) taken to c classes: a row a_t of features has the scores z_t = W a_t, W [c][d].
+ * Types of the features and of the model (one for both, and for their gradients): float32, float16, bfloat16.  Sums, scores,
+ * probabilities and losses are float32 throughout; products of float32 are carried out to float32's own precision on the matrix
+ * cores, in three bfloat16 parts (magnitudes of 2^127 * 1.99 and more count as infinite; anything not finite gives losses that
+ * are not finite). */
+#define DQ_F32   0
+#define DQ_F16   1
+#define DQ_BF16  2
+
+/* Host struct: n rows of features and a model of c classes, both d wide; lda, ldw: elements from one row to the next (>= d; any,
+ * as any alignment to the element, but rows that are 16-byte aligned with d % 32 == 0 are read in place). */
+typedef struct dq_classes {
+    int32_t type;                    /* DQ_F32, DQ_F16, DQ_BF16 */
+    int64_t n, c, d;
+    const void *a; int64_t lda;
+    const void *w; int64_t ldw;
+} dq_classes;
+
+/* Host struct: a teacher's largest logits.  Row t's entries are cls[t*ld + j], logit[t*ld + j], j < k, in any order; a class below 0
+ * is an entry that is not there.  A class that comes twice counts twice.  tau > 0: the temperature. */
+typedef struct dq_teacher {
+    int64_t k;
+    const int32_t *cls;
+    const float *logit;
+    int64_t ld;
+    float tau;
+} dq_teacher;
+#define DQ_MAX_TEACHER 1024          /* largest k */
+
+#define DQ_OP_CLASS_LOSS  4   /* dq_class_loss, dq_distill_loss */
+#define DQ_OP_CLASS_GRAD  5   /* dq_class_grad, dq_distill_grad */
+/* Bytes of workspace of `op`, as dq_workspace_bytes; k: the teacher's, 0 for labels.  The scores of all classes are never kept:
+ * the gradients take the classes in pieces whose n columns of gradients fit 512 MB. */
+int64_t dq_class_workspace_bytes(int32_t op, const dq_classes *prob /*host*/, int64_t k);
+
+/* Softmax cross entropy: loss_out[t] = lse_t - z_t,label[t],  lse_t = log sum_j exp z_tj  (lse_out nullable).
+ * A row with a label below 0 is left out: its loss is 0 (its lse is still written).  A label of c or more leaves the row out too and
+ * sets status bit 1.  Status bit 0: the lse of a row that is not left out is not finite. */
+int32_t dq_class_loss(const dq_classes *prob /*host*/, const int32_t *label, float *loss_out, float *lse_out,
+                      uint32_t *status, void *ws, int64_t ws_bytes, void *stream);
+
+/* The same losses, and the gradients of  scale * sum_t weight[t] loss_t  (weight nullable: all 1):
+ *   g_tj = scale weight_t (softmax(z_t)_j - [j = label_t]),   da_out = g W  [n][ldda],   dw_out = g^T a  [c][lddw],
+ * either nullable, of the problem's type, whole (rows left out: zeros in da_out, nothing to dw_out, whatever the row holds).
+ * loss_out, lse_out nullable.  Deterministic: sums in a fixed order.  g itself is rounded to the problem's type (float32: kept
+ * whole) for the two products: by at most 2^-8 or 2^-11 of each term; in float16 as a multiple of the largest |weight| that keeps terms
+ * down to 2^-29 of it normal.  The outputs must not overlap the inputs. */
+int32_t dq_class_grad(const dq_classes *prob /*host*/, const int32_t *label, const float *weight, float scale,
+                      float *loss_out, float *lse_out, void *da_out, int64_t ldda, void *dw_out, int64_t lddw,
+                      uint32_t *status, void *ws, int64_t ws_bytes, void *stream);
+
+/* Distillation: with q_t = softmax(logit_t / tau) over the entries of row t and p_t = softmax(z_t / tau) over all classes,
+ *   loss_out[t] = tau^2 sum_j q_tj (log q_tj - log p_tj),   lse_out[t] = log sum_j exp(z_tj / tau).
+ * A row without an entry (or whose logits are all -inf) is left out, as above.  Entries with a class of c or more are not there, and
+ * set status bit 1. */
+int32_t dq_distill_loss(const dq_classes *prob /*host*/, const dq_teacher *teacher /*host*/, float *loss_out, float *lse_out,
+                        uint32_t *status, void *ws, int64_t ws_bytes, void *stream);
+/* The same with gradients:  g_tj = scale weight_t tau (p_tj - q_tj). */
+int32_t dq_distill_grad(const dq_classes *prob /*host*/, const dq_teacher *teacher /*host*/, const float *weight, float scale,
+                        float *loss_out, float *lse_out, void *da_out, int64_t ldda, void *dw_out, int64_t lddw,
+                        uint32_t *status, void *ws, int64_t ws_bytes, void *stream);
+
+/* ---- models in 4 bits --------------------------------------------------------------- */
+
+/* A matrix in microscaled 4-bit numbers (the (delta, b) idea with one power-of-two scale per 32 neighbours, and levels that the
+ * matrix cores multiply): value = level * 2^(scale - 127), level one of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} (code: sign bit 8, the
+ * level's number below it).  A row of d numbers is stored in whole groups of 128: dq_mx4_row_bytes(d) bytes of codes (number 2i in
+ * the low half of byte i) and dq_mx4_row_scales(d) bytes of scales, codes behind the row's end zero, their scales finite (not 255;
+ * dq_mx4_quantize writes 0).  codes 16-byte aligned with ld_codes % 16 == 0, scales 4-byte aligned with ld_scales % 4 == 0. */
+typedef struct dq_mx4 {
+    int64_t n, d;
+    uint8_t *codes; int64_t ld_codes;
+    uint8_t *scales; int64_t ld_scales;
+} dq_mx4;
+int64_t dq_mx4_row_bytes(int64_t d);
+int64_t dq_mx4_row_scales(int64_t d);
+
+/* q = v rounded, v [q.n][ld] of `type`, q.d wide: scale exponent floor(log2 of the block's largest magnitude) - 2, at least -127; each
+ * number to the nearest level, ties to the even code, beyond 6 to 6.  A block with an infinity or a NaN gets scale 255 (all its
+ * values are NaN) and sets status bit 0.  Its gradient in training is taken straight through (the identity). */
+int32_t dq_mx4_quantize(const void *v, int32_t type, int64_t ld, const dq_mx4 *q /*host*/, uint32_t *status, void *stream);
+/* out = the values of q (exact in every type for scales that the type can hold, else rounded once). */
+int32_t dq_mx4_dequantize(const dq_mx4 *q /*host*/, void *out, int32_t type, int64_t ld, void *stream);
+
+/* out[t][j] = sum_i a_ti w_ji over a.d = w.d, products exact, sums float32: [a.n][ld] of `type`. */
+int32_t dq_mx4_product(const dq_mx4 *a /*host*/, const dq_mx4 *w /*host*/, void *out, int32_t type, int64_t ld, void *stream);
+
+/* Scores of n rows against a model in 4 bits: dq_mx4_quantize of the rows, then dq_mx4_product, `type` and `out_type` their types.
+ * ws: at least dq_mx4_scores_bytes(n, w.d) bytes. */
+int64_t dq_mx4_scores_bytes(int64_t n, int64_t d);
+int32_t dq_mx4_scores(const void *a, int32_t type, int64_t n, int64_t lda, const dq_mx4 *w /*host*/, void *out, int32_t out_type,
+                      int64_t ld, uint32_t *status, void *ws, int64_t ws_bytes, void *stream);
 
 /* ---- message sizes ---------------------------------------------------------------- */
 

@@ -59,6 +59,20 @@ class RunState(C.Structure):
                 ("xq_stride_words", C.c_int64), ("wire", C.c_void_p), ("ld_wire", C.c_int64), ("wire_nnz", C.c_void_p)]
 
 
+class _Classes(C.Structure):
+    _fields_ = [("type", C.c_int32), ("n", C.c_int64), ("c", C.c_int64), ("d", C.c_int64),
+                ("a", C.c_void_p), ("lda", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64)]
+
+
+class _Teacher(C.Structure):
+    _fields_ = [("k", C.c_int64), ("cls", C.c_void_p), ("logit", C.c_void_p), ("ld", C.c_int64), ("tau", C.c_float)]
+
+
+class _Mx4(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d", C.c_int64), ("codes", C.c_void_p), ("ld_codes", C.c_int64),
+                ("scales", C.c_void_p), ("ld_scales", C.c_int64)]
+
+
 ALGO = {"asylpg": 0, "sparse": 1, "acc": 2}
 
 _vp, _i64, _i32, _u64, _u32, _f32 = C.c_void_p, C.c_int64, C.c_int32, C.c_uint64, C.c_uint32, C.c_float
@@ -95,6 +109,18 @@ _SIGS = {
     "dq_sparse_encode": (_i32, [_vp, _i64, _i64, _i64, _i32, _vp, _i64, _vp, _vp]),
     "dq_sparse_decode": (_i32, [_vp, _i64, _vp, _i64, _i64, _i32, _vp, _i64, _vp]),
     "dq_mu_terms": (_i32, [_vp, _vp, _i64, _i32, _vp, _vp]),
+    "dq_class_workspace_bytes": (_i64, [_i32, _vp, _i64]),
+    "dq_class_loss": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "dq_class_grad": (_i32, [_vp, _vp, _vp, _f32, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp]),
+    "dq_distill_loss": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "dq_distill_grad": (_i32, [_vp, _vp, _vp, _f32, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp]),
+    "dq_mx4_row_bytes": (_i64, [_i64]),
+    "dq_mx4_row_scales": (_i64, [_i64]),
+    "dq_mx4_quantize": (_i32, [_vp, _i32, _i64, _vp, _vp, _vp]),
+    "dq_mx4_dequantize": (_i32, [_vp, _vp, _i32, _i64, _vp]),
+    "dq_mx4_product": (_i32, [_vp, _vp, _vp, _i32, _i64, _vp]),
+    "dq_mx4_scores_bytes": (_i64, [_i64, _i64]),
+    "dq_mx4_scores": (_i32, [_vp, _i32, _i64, _i64, _vp, _vp, _i32, _i64, _vp, _vp, _i64, _vp]),
     "dq_run_rounds": (_i32, [_vp, _vp, _vp, _i64, _i64, _i64, _f32, _f32, _vp, _vp]),
 }
 
@@ -409,6 +435,202 @@ def dq_mu_terms(x, x_snap, b, out) -> None:
                                            _ptr(out, torch.float64, "out"), _stream()))
 
 
+# ------------------------------------------------------------------ models of many classes
+OP_CLASS_LOSS, OP_CLASS_GRAD = 4, 5
+MAX_TEACHER = 1024
+TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _matrix(t: torch.Tensor, name: str, dtype=None, shape=None):
+    """(pointer, row stride) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return _ptr(t, dtype, name), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _vector(t: Optional[torch.Tensor], dtype, name: str, n: int):
+    if t is not None and (t.shape != (n,) or (n > 1 and t.stride(0) != 1)):
+        raise ValueError(f"{name} must be {n} contiguous values")
+    return _ptr(t, dtype, name)
+
+
+@dataclass
+class DeviceClasses:
+    """Rows of features and a model of many classes (one type for both); keeps its tensors alive."""
+
+    a: torch.Tensor      # [n, d]
+    w: torch.Tensor      # [c, d]
+
+    def __post_init__(self):
+        if self.a.dtype not in TYPES or self.w.dtype != self.a.dtype:
+            raise TypeError(f"features and model must both be float32, float16 or bfloat16, got {self.a.dtype} and {self.w.dtype}")
+        s = _Classes()
+        s.type = TYPES[self.a.dtype]
+        s.a, s.lda = _matrix(self.a, "a")
+        s.w, s.ldw = _matrix(self.w, "w")
+        if self.a.shape[1] != self.w.shape[1]:
+            raise ValueError(f"features are {self.a.shape[1]} wide, the model {self.w.shape[1]}")
+        s.n, s.c, s.d = self.a.shape[0], self.w.shape[0], self.a.shape[1]
+        self._s = s
+
+    @property
+    def ptr(self):
+        return C.addressof(self._s)
+
+
+@dataclass
+class Teacher:
+    """A teacher's largest logits a row: cls [n, k] int32 (below 0: no entry), logit [n, k] float32, temperature tau."""
+
+    cls: torch.Tensor
+    logit: torch.Tensor
+    tau: float = 1.0
+
+    def __post_init__(self):
+        s = _Teacher()
+        s.cls, s.ld = _matrix(self.cls, "cls", torch.int32)
+        s.logit, ld = _matrix(self.logit, "logit", torch.float32, self.cls.shape)
+        if ld != s.ld:
+            raise ValueError("cls and logit must have the same row stride")
+        s.k, s.tau = self.cls.shape[1], self.tau
+        self._s = s
+
+    @property
+    def ptr(self):
+        return C.addressof(self._s)
+
+
+def dq_class_workspace_bytes(op: int, prob: DeviceClasses, k: int = 0) -> int:
+    return int(_lib.dq_class_workspace_bytes(op, prob.ptr, k))
+
+
+def new_class_workspace(op: int, prob: DeviceClasses, target=None) -> torch.Tensor:
+    """Allocates a workspace for `op`; target: the labels or the Teacher of the calls."""
+    nbytes = dq_class_workspace_bytes(op, prob, target.cls.shape[1] if isinstance(target, Teacher) else 0)
+    if nbytes < 0:
+        raise DqError("dq_class_workspace_bytes", nbytes)
+    return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=prob.a.device)
+
+
+def _rows_of(prob: DeviceClasses, target):
+    """The pointer that names the targets: labels or a Teacher."""
+    if isinstance(target, Teacher):
+        if target.cls.shape[0] != prob.a.shape[0]:
+            raise ValueError(f"the teacher has {target.cls.shape[0]} rows, the problem {prob.a.shape[0]}")
+        return target.ptr
+    return _vector(target, torch.int32, "label", prob.a.shape[0])
+
+
+def _class_loss(name, prob, target, loss_out, lse_out, status, ws):
+    n, (wp, wb) = prob.a.shape[0], _ws(ws)
+    _check(name, getattr(_lib, name)(prob.ptr, _rows_of(prob, target), _vector(loss_out, torch.float32, "loss_out", n),
+                                     _vector(lse_out, torch.float32, "lse_out", n), _ptr(status, torch.int32, "status"), wp, wb, _stream()))
+
+
+def _class_grad(name, prob, target, weight, scale, loss_out, lse_out, da_out, dw_out, status, ws):
+    n, t, (wp, wb) = prob.a.shape[0], prob.a.dtype, _ws(ws)
+    da = (None, 0) if da_out is None else _matrix(da_out, "da_out", t, prob.a.shape)
+    dw = (None, 0) if dw_out is None else _matrix(dw_out, "dw_out", t, prob.w.shape)
+    _check(name, getattr(_lib, name)(prob.ptr, _rows_of(prob, target), _vector(weight, torch.float32, "weight", n), scale,
+                                     _vector(loss_out, torch.float32, "loss_out", n), _vector(lse_out, torch.float32, "lse_out", n),
+                                     *da, *dw, _ptr(status, torch.int32, "status"), wp, wb, _stream()))
+
+
+def dq_class_loss(prob: DeviceClasses, label, loss_out, lse_out=None, status=None, ws=None) -> None:
+    _class_loss("dq_class_loss", prob, label, loss_out, lse_out, status, ws)
+
+
+def dq_class_grad(prob: DeviceClasses, label, weight, scale, loss_out, lse_out, da_out, dw_out, status=None, ws=None) -> None:
+    _class_grad("dq_class_grad", prob, label, weight, scale, loss_out, lse_out, da_out, dw_out, status, ws)
+
+
+def dq_distill_loss(prob: DeviceClasses, teacher: Teacher, loss_out, lse_out=None, status=None, ws=None) -> None:
+    _class_loss("dq_distill_loss", prob, teacher, loss_out, lse_out, status, ws)
+
+
+def dq_distill_grad(prob: DeviceClasses, teacher: Teacher, weight, scale, loss_out, lse_out, da_out, dw_out, status=None, ws=None) -> None:
+    _class_grad("dq_distill_grad", prob, teacher, weight, scale, loss_out, lse_out, da_out, dw_out, status, ws)
+
+
+# ------------------------------------------------------------------ models in 4 bits
+def dq_mx4_row_bytes(d: int) -> int:
+    return int(_lib.dq_mx4_row_bytes(d))
+
+
+def dq_mx4_row_scales(d: int) -> int:
+    return int(_lib.dq_mx4_row_scales(d))
+
+
+@dataclass
+class Mx4:
+    """A matrix [n, d] in 4-bit codes with a scale per 32 numbers: codes [n, dq_mx4_row_bytes(d)], scales [n, dq_mx4_row_scales(d)], uint8."""
+
+    codes: torch.Tensor
+    scales: torch.Tensor
+    d: int
+
+    def __post_init__(self):
+        s = _Mx4()
+        n = self.codes.shape[0]
+        s.codes, s.ld_codes = _matrix(self.codes, "codes", torch.uint8, (n, dq_mx4_row_bytes(self.d)))
+        s.scales, s.ld_scales = _matrix(self.scales, "scales", torch.uint8, (n, dq_mx4_row_scales(self.d)))
+        s.n, s.d = n, self.d
+        self._s = s
+
+    @property
+    def n(self) -> int:
+        return self.codes.shape[0]
+
+    @property
+    def ptr(self):
+        return C.addressof(self._s)
+
+
+def new_mx4(n: int, d: int, device="cuda") -> Mx4:
+    """Room for an [n, d] matrix in 4 bits (not initialised)."""
+    u8 = dict(dtype=torch.uint8, device=device)
+    return Mx4(torch.empty((n, dq_mx4_row_bytes(d)), **u8), torch.empty((n, dq_mx4_row_scales(d)), **u8), d)
+
+
+def _typed(t: torch.Tensor, name: str, shape):
+    """(pointer, type, row stride) of a matrix of one of the three types."""
+    if t.dtype not in TYPES:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
+    p, ld = _matrix(t, name, None, shape)
+    return p, TYPES[t.dtype], ld
+
+
+def dq_mx4_quantize(v, q: Mx4, status=None) -> None:
+    p, t, ld = _typed(v, "v", (q.n, q.d))
+    _check("dq_mx4_quantize", _lib.dq_mx4_quantize(p, t, ld, q.ptr, _ptr(status, torch.int32, "status"), _stream()))
+
+
+def dq_mx4_dequantize(q: Mx4, out) -> None:
+    _check("dq_mx4_dequantize", _lib.dq_mx4_dequantize(q.ptr, *_typed(out, "out", (q.n, q.d)), _stream()))
+
+
+def dq_mx4_product(a: Mx4, w: Mx4, out) -> None:
+    _check("dq_mx4_product", _lib.dq_mx4_product(a.ptr, w.ptr, *_typed(out, "out", (a.n, w.n)), _stream()))
+
+
+def dq_mx4_scores_bytes(n: int, d: int) -> int:
+    return int(_lib.dq_mx4_scores_bytes(n, d))
+
+
+def new_scores_workspace(n: int, d: int, device="cuda") -> torch.Tensor:
+    """Allocates the workspace of dq_mx4_scores for n rows."""
+    return torch.empty(max(dq_mx4_scores_bytes(n, d), 16), dtype=torch.uint8, device=device)
+
+
+def dq_mx4_scores(a, w: Mx4, out, status=None, ws=None) -> None:
+    p, t, ld = _typed(a, "a", (a.shape[0], w.d))
+    wp, wb = _ws(ws)
+    _check("dq_mx4_scores", _lib.dq_mx4_scores(p, t, a.shape[0], ld, w.ptr, *_typed(out, "out", (a.shape[0], w.n)),
+                                               _ptr(status, torch.int32, "status"), wp, wb, _stream()))
+
+
 def dq_run_rounds(prob: DeviceProblem, cfg: RunConfig, state: RunState, epoch: int, t0: int, rounds: int,
                   eta: float, theta: float, worker_events=None) -> None:
     """worker_events: optional list of 2*rounds raw hipEvent_t handles (ints; None for a round without events)."""
@@ -427,5 +649,9 @@ __all__ = [
     "dq_version", "dq_last_device_error", "dq_workspace_bytes", "dq_workspace_init", "new_workspace", "dq_absmax", "dq_quantize", "dq_dequantize",
     "dq_pack", "dq_unpack", "dq_quantize_pack", "dq_unpack_dequant_sum", "dq_sample_indices", "dq_full_grad",
     "dq_vr_grad", "dq_sparsify", "dq_worker_step", "dq_worker_step_static", "STATIC_WS_BYTES", "dq_master_step", "dq_master_step_each", "dq_acc_mix", "dq_acc_snapshot",
+    "OP_CLASS_LOSS", "OP_CLASS_GRAD", "MAX_TEACHER", "DeviceClasses", "Teacher", "dq_class_workspace_bytes", "new_class_workspace",
+    "dq_class_loss", "dq_class_grad", "dq_distill_loss", "dq_distill_grad",
+    "Mx4", "new_mx4", "dq_mx4_row_bytes", "dq_mx4_row_scales", "dq_mx4_quantize", "dq_mx4_dequantize", "dq_mx4_product",
+    "dq_mx4_scores_bytes", "new_scores_workspace", "dq_mx4_scores",
     "dq_run_rounds", "dq_mu_terms", "dq_acc_params", "dq_message_bits", "MSG_DENSE", "MSG_FLAG", "MSG_SPARSE", "dq_sparse_stream_words", "dq_sparse_encode", "dq_sparse_decode", "RunConfig", "RunState", "ALGO",
 ]

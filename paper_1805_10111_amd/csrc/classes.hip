@@ -1,0 +1,692 @@
+// Models of many classes: softmax cross entropy and distillation from a teacher's largest logits, with gradients.
+//
+// Both losses are sums  entropy_t + sum_j q_tj (lse_t - z_tj)  over a row's few targets (class, q): a label is one target of weight 1.
+// The scores z = a W^T / tau are made tile by tile and never stored:
+//   targets   the rows' targets in order of class, their weights q, which rows take part
+//   scores    one tile of z: per row its maximum, the sum of exp above it and the targets' sum q z
+//   finish    lse and loss of a row from its tiles
+//   grad      (a piece of the classes at a time) the tile again, now g = f (exp(z - lse) - q), rounded to 16 bits
+//   da        += g W of the piece, split over its classes where there are few tiles
+//   dw        = g^T a of the piece
+#include <algorithm>
+
+#include "dq_common.h"
+#include "matrix_tile.h"
+
+namespace dq {
+
+constexpr int kNoClass = 0x7fffffff;
+constexpr int64_t kPieceBytes = 512ll << 20;   // of g
+constexpr float kF16Unit = 16384.0f;           // g of float16: terms down to 2^-29 of the largest weight stay normal
+
+// The three bfloat16 whose sum is v.  Infinities and NaNs: the first part alone.
+__device__ __forceinline__ void parts_of(float v, u16 out[3])
+{
+    out[0] = Part::store(v);
+    const float r = v - Part::load(out[0]);
+    const bool whole = __builtin_isfinite(Part::load(out[0]));
+    out[1] = whole ? Part::store(r) : 0;
+    out[2] = whole ? Part::store(r - Part::load(out[1])) : 0;
+}
+
+// ---- operands that are not read in place ---------------------------------------
+// Rows of [rows][cols] to rows of out_cols 16-bit numbers (three planes of them for float32), zeros behind row and column ends, and
+// in rows without a target where `cls` is given.  One thread per eight columns.
+template <int TYPE>
+__global__ __launch_bounds__(256) void pack_rows_kernel(const typename Num<TYPE>::Mem *__restrict__ v, int64_t ld, int64_t rows,
+                                                        int64_t cols, u16 *__restrict__ out, int64_t out_cols, int64_t out_rows,
+                                                        const int32_t *__restrict__ cls, int64_t k)
+{
+    const int64_t each = out_cols / 8, total = out_rows * each;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+        const int64_t r = i / each, c = (i - r * each) * 8;
+        const bool live = r < rows && (!cls || cls[r * k] != kNoClass);
+        u16 part[3][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool in = live && c + e < cols;
+            if constexpr (TYPE == DQ_F32) {
+                u16 p[3];
+                parts_of(in ? v[r * ld + c + e] : 0.0f, p);
+                part[0][e] = p[0];
+                part[1][e] = p[1];
+                part[2][e] = p[2];
+            } else {
+                part[0][e] = in ? v[r * ld + c + e] : 0;
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < (TYPE == DQ_F32 ? 3 : 1); ++p)
+            *reinterpret_cast<i32x4 *>(out + p * out_rows * out_cols + r * out_cols + c) = __builtin_bit_cast(i32x4, part[p]);
+    }
+}
+
+// ---- targets -------------------------------------------------------------------
+__global__ __launch_bounds__(256) void label_kernel(const int32_t *__restrict__ label, int64_t n, int64_t c, int32_t *__restrict__ cls,
+                                                    uint32_t *__restrict__ status)
+{
+    const int64_t t = blockIdx.x * 256ll + threadIdx.x;
+    if (t >= n) return;
+    const int32_t l = label[t];
+    if (l >= c && status) atomicOr(status, 2u);
+    cls[t] = l >= 0 && l < c ? l : kNoClass;
+}
+
+// The largest |weight| of a call in float16, one block.
+__global__ __launch_bounds__(1024) void weight_max_kernel(const float *__restrict__ weight, int64_t n, float *__restrict__ out)
+{
+    __shared__ uint32_t top;
+    if (threadIdx.x == 0) top = 0;
+    __syncthreads();
+    uint32_t m = 0;
+    for (int64_t t = threadIdx.x; t < n; t += 1024) m = max(m, __float_as_uint(weight[t]) & 0x7fffffffu);
+    atomicMax(&top, m);
+    __syncthreads();
+    if (threadIdx.x == 0) out[0] = top ? __uint_as_float(top) : 1.0f;
+}
+
+// One block of 64 threads per row: q = softmax(logit / tau) over the entries, sorted by class (bitonic, in LDS).
+// entropy[t] = sum q log q.  Rows without an entry: all classes kNoClass.
+constexpr int kTeacherThreads = 64;
+__global__ __launch_bounds__(kTeacherThreads) void teacher_kernel(const int32_t *__restrict__ cls_in, const float *__restrict__ logit, int64_t ld,
+                                                                  int k, int pow2, int64_t c, float inv_tau, int32_t *__restrict__ cls,
+                                                                  float *__restrict__ q, float *__restrict__ entropy,
+                                                                  uint32_t *__restrict__ status)
+{
+    __shared__ int32_t key[DQ_MAX_TEACHER];
+    __shared__ float val[DQ_MAX_TEACHER];
+    const int64_t t = blockIdx.x;
+    const int lane = threadIdx.x;
+    bool far = false;
+    float top = -INFINITY;
+    for (int j = lane; j < pow2; j += kTeacherThreads) {
+        int32_t x = j < k ? cls_in[t * ld + j] : -1;
+        if (x >= c) far = true;
+        if (x < 0 || x >= c) x = kNoClass;
+        const float u = x == kNoClass ? -INFINITY : logit[t * ld + j] * inv_tau;
+        key[j] = x;
+        val[j] = u;
+        top = u > top || u != u ? u : top;
+    }
+    if (far && status) atomicOr(status, 2u);
+    for (int o = 32; o; o >>= 1) {
+        const float other = __shfl_xor(top, o);
+        top = other > top || other != other ? other : top;
+    }
+    const bool none = top == -INFINITY;
+    float sum = 0.0f;
+    for (int j = lane; j < pow2; j += kTeacherThreads) {
+        if (none) key[j] = kNoClass;
+        else if (key[j] != kNoClass) sum += expf(val[j] - top);
+    }
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    const float log_sum = logf(sum);
+    float ent = 0.0f;
+    for (int j = lane; j < pow2; j += kTeacherThreads) {
+        const float l = val[j] - top, p = key[j] == kNoClass ? 0.0f : expf(l) / sum;
+        val[j] = p;
+        ent += p == 0.0f ? 0.0f : p * (l - log_sum);
+    }
+    for (int o = 32; o; o >>= 1) ent += __shfl_xor(ent, o);
+    if (lane == 0) entropy[t] = none ? 0.0f : ent;
+    __syncthreads();
+    for (int size = 2; size <= pow2; size *= 2)
+        for (int step = size / 2; step; step /= 2) {
+            for (int i = lane; i < pow2 / 2; i += kTeacherThreads) {
+                const int a = i / step * step * 2 + i % step, b = a + step;
+                const bool up = !(a & size);
+                const int32_t ka = key[a], kb = key[b];
+                if (up ? ka > kb : ka < kb) {
+                    key[a] = kb;
+                    key[b] = ka;
+                    const float v = val[a];
+                    val[a] = val[b];
+                    val[b] = v;
+                }
+            }
+            __syncthreads();
+        }
+    for (int j = lane; j < k; j += kTeacherThreads) {
+        cls[t * k + j] = key[j];
+        q[t * k + j] = val[j];
+    }
+}
+
+// What the tile kernels know of the rows' targets: k per row, sorted by class, q null for labels.
+struct Targets {
+    const int32_t *cls;
+    const float *q;
+    int32_t k;
+};
+
+// first target of row t with a class of at least c0
+__device__ __forceinline__ int first_target(const Targets &g, int64_t t, int c0)
+{
+    const int32_t *cls = g.cls + t * g.k;
+    int lo = 0, hi = g.k;
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (cls[mid] < c0) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// ---- scores --------------------------------------------------------------------
+__device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+// Sums of a tile's row are kept per wavefront column (slot): the row's maximum, the sum of exp above it, the targets' sum q z.
+template <int TYPE, int XT, int YT, int WX, int WY>
+__global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operand a, int64_t k, int steps, int64_t n, int64_t c,
+                                                               float inv_tau, Targets targets, int tiles_x, int tiles_y,
+                                                               float2 *__restrict__ sums, float *__restrict__ hits)
+{
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false> Tile;
+    int tx, ty;
+    tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
+    const int64_t c0 = static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
+    Tile tile;
+    tile.run(w, a, c0, t0, 0, k, steps);
+    const int lane = threadIdx.x & 63, wave_c0 = static_cast<int>(c0) + Tile::sub_x(0) * 16;
+    const int64_t slot = static_cast<int64_t>(tx) * WX + Tile::wave() % WX;
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) {
+        const int64_t t = t0 + Tile::at_y(y);
+        const bool live = t < n;
+        const int base = static_cast<int>(c0) + Tile::at_x(0);
+        float top = -INFINITY;
+#pragma unroll
+        for (int m = 0; m < Tile::SX; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float z = base + 16 * m + i < c ? tile.acc[m][y][i] * inv_tau : -INFINITY;
+                tile.acc[m][y][i] = z;
+                top = fmaxf(top, z);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        float sum = 0.0f;
+        const float from = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int m = 0; m < Tile::SX; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += TYPE == DQ_F32 ? expf(tile.acc[m][y][i] - from) : exp_near(tile.acc[m][y][i] - from);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        float hit = 0.0f;
+        if (live) {
+            const int end = min(wave_c0 + Tile::SX * 16, static_cast<int>(c));
+            const int32_t *cls = targets.cls + t * targets.k;
+            for (int e = first_target(targets, t, wave_c0); e < targets.k && cls[e] < end; ++e) {
+                const int rel = cls[e] - base;
+                const float q = targets.q ? targets.q[t * targets.k + e] : 1.0f;
+                float z = 0.0f;
+#pragma unroll
+                for (int m = 0; m < Tile::SX; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z = rel == 16 * m + i ? tile.acc[m][y][i] : z;
+                hit += q == 0.0f ? 0.0f : q * z;
+            }
+        }
+        hit += __shfl_xor(hit, 16);
+        hit += __shfl_xor(hit, 32);
+        if (live && lane < 16) {
+            sums[slot * n + t] = make_float2(top, sum);
+            hits[slot * n + t] = hit;
+        }
+    }
+}
+
+// Sixteen rows a block, sixteen threads a row.
+__global__ __launch_bounds__(256) void finish_kernel(const float2 *__restrict__ sums, const float *__restrict__ hits, int slots, int64_t n,
+                                                     const int32_t *__restrict__ cls, int32_t k, const float *__restrict__ entropy,
+                                                     float tau2, float *__restrict__ loss, float *__restrict__ lse_out,
+                                                     float *__restrict__ lse_kept, uint32_t *__restrict__ status)
+{
+    __shared__ float3 shared[16][16];
+    const int row = threadIdx.x & 15, part = threadIdx.x >> 4;
+    const int64_t t = blockIdx.x * 16ll + row;
+    float top = -INFINITY, sum = 0.0f, hit = 0.0f;
+    if (t < n)
+        for (int s = part; s < slots; s += 16) {
+            const float2 v = sums[s * n + t];
+            const float m = fmaxf(top, v.x), from = m == -INFINITY ? 0.0f : m;
+            sum = sum * expf(top - from) + v.y * expf(v.x - from);
+            top = m;
+            hit += hits[s * n + t];
+        }
+    shared[part][row] = make_float3(top, sum, hit);
+    __syncthreads();
+    if (part || t >= n) return;
+    for (int p = 1; p < 16; ++p) {
+        const float3 v = shared[p][row];
+        const float m = fmaxf(top, v.x), from = m == -INFINITY ? 0.0f : m;
+        sum = sum * expf(top - from) + v.y * expf(v.x - from);
+        top = m;
+        hit += v.z;
+    }
+    const float lse = top + logf(sum);
+    const bool live = cls[t * k] != kNoClass;
+    if (loss) loss[t] = live ? tau2 * ((entropy ? entropy[t] : 0.0f) + (lse - hit)) : 0.0f;
+    if (lse_out) lse_out[t] = lse;
+    if (lse_kept) lse_kept[t] = lse;
+    if (live && status && !__builtin_isfinite(lse)) atomicOr(status, 1u);
+}
+
+// ---- gradients -----------------------------------------------------------------
+// g of a piece of the classes, [rows of the tiles][ldg] in 16 bits (three planes for float32); zeros where there is no row or class.
+template <int TYPE, int XT, int YT, int WX, int WY>
+__global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand a, int64_t k, int steps, int64_t n, int64_t c, int64_t piece0,
+                                                             int64_t piece, float inv_tau, Targets targets, const float *__restrict__ lse,
+                                                             const float *__restrict__ weight, const float *__restrict__ weight_max,
+                                                             int tiles_x, int tiles_y, u16 *__restrict__ g, int64_t ldg, int64_t plane)
+{
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false> Tile;
+    int tx, ty;
+    tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
+    const int64_t c0 = piece0 + static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
+    Tile tile;
+    tile.run(w, a, c0, t0, 0, k, steps);
+    const int wave_c0 = static_cast<int>(c0) + Tile::sub_x(0) * 16;
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) {
+        const int64_t t = t0 + Tile::at_y(y);
+        const bool live = t < n && targets.cls[t * targets.k] != kNoClass;
+        const int base = static_cast<int>(c0) + Tile::at_x(0);
+        const float from = live ? lse[t] : 0.0f;
+        float f = live && weight ? weight[t] : 1.0f;
+        if constexpr (TYPE == DQ_F16) f = f * (kF16Unit / (weight ? weight_max[0] : 1.0f));
+#pragma unroll
+        for (int m = 0; m < Tile::SX; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float z = tile.acc[m][y][i] * inv_tau - from;
+                tile.acc[m][y][i] = TYPE == DQ_F32 ? expf(z) : exp_near(z);
+            }
+        if (live) {
+            const int end = min(wave_c0 + Tile::SX * 16, static_cast<int>(c));
+            const int32_t *cls = targets.cls + t * targets.k;
+            for (int e = first_target(targets, t, wave_c0); e < targets.k && cls[e] < end; ++e) {
+                const int rel = cls[e] - base;
+                const float q = targets.q ? targets.q[t * targets.k + e] : 1.0f;
+#pragma unroll
+                for (int m = 0; m < Tile::SX; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tile.acc[m][y][i] -= rel == 16 * m + i ? q : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < Tile::SX; ++m) {
+            u16 part[3][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v = live && base + 16 * m + i < c ? f * tile.acc[m][y][i] : 0.0f;
+                if constexpr (TYPE == DQ_F32) {
+                    u16 p[3];
+                    parts_of(v, p);
+                    part[0][i] = p[0];
+                    part[1][i] = p[1];
+                    part[2][i] = p[2];
+                } else {
+                    part[0][i] = Num<TYPE>::store(v);
+                }
+            }
+            u16 *const to = g + t * ldg + (base + 16 * m - piece0);
+#pragma unroll
+            for (int p = 0; p < (TYPE == DQ_F32 ? 3 : 1); ++p)
+                *reinterpret_cast<u16x4 *>(to + p * plane) = u16x4{part[p][0], part[p][1], part[p][2], part[p][3]};
+        }
+    }
+}
+
+__device__ __forceinline__ float gradient_unit(int type, float post, const float *weight_max)
+{
+    return type == DQ_F16 ? post * ((weight_max ? weight_max[0] : 1.0f) / kF16Unit) : post;
+}
+
+// da of a piece, one split of its classes per blockIdx.y: partial sums [split][n][ldp] in float32, added to what the pieces before left.
+template <int TYPE, int XT, int YT, int WX, int WY>
+__global__ __launch_bounds__(WX *WY *kWave) void da_kernel(Operand w, Operand g, int64_t piece, int64_t per_split, int steps, int64_t n, int tiles_x,
+                                                           int tiles_y, float *__restrict__ partial, int64_t ldp, int first)
+{
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, false> Tile;
+    int tx, ty;
+    tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
+    const int64_t i0 = static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT, k0 = blockIdx.y * per_split;
+    const int64_t k1 = min(k0 + per_split, piece);
+    if (k0 >= k1 && !first) return;
+    Tile tile;
+    tile.run(w, g, i0, t0, k0, max(k0, k1), steps);
+    float *const out = partial + blockIdx.y * n * ldp;
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) {
+        const int64_t t = t0 + Tile::at_y(y);
+        if (t >= n) continue;
+#pragma unroll
+        for (int m = 0; m < Tile::SX; ++m) {
+            const int64_t i = i0 + Tile::at_x(m);
+            if (i >= ldp) continue;
+            f32x4 *const to = reinterpret_cast<f32x4 *>(out + t * ldp + i);
+            *to = first ? tile.acc[m][y] : *to + tile.acc[m][y];
+        }
+    }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(256) void da_finish_kernel(const float *__restrict__ partial, int splits, int64_t n, int64_t d, int64_t ldp,
+                                                        const int32_t *__restrict__ cls, int32_t k, float post,
+                                                        const float *__restrict__ weight_max, typename Num<TYPE>::Mem *__restrict__ da,
+                                                        int64_t ldda, int vector)
+{
+    const int64_t quads = (d + 3) / 4, total = n * quads;
+    const float unit = gradient_unit(TYPE, post, weight_max);
+    for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < total; at += gridDim.x * 256ll) {
+        const int64_t t = at / quads, i = (at - t * quads) * 4;
+        f32x4 v{0.f, 0.f, 0.f, 0.f};
+        if (cls[t * k] != kNoClass) {
+            for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x4 *>(partial + (s * n + t) * ldp + i);
+            v *= unit;
+        }
+        store_four<TYPE>(da + t * ldda + i, v, static_cast<int>(min<int64_t>(4, d - i)), vector);
+    }
+}
+
+template <int TYPE, int XT, int YT, int WX, int WY>
+__global__ __launch_bounds__(WX *WY *kWave) void dw_kernel(Operand a, Operand g, int64_t k, int steps, int64_t piece, int64_t d, int tiles_x, int tiles_y,
+                                                           float post, const float *__restrict__ weight_max,
+                                                           typename Num<TYPE>::Mem *__restrict__ dw, int64_t lddw, int vector)
+{
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, true> Tile;
+    int tx, ty;
+    tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
+    const int64_t i0 = static_cast<int64_t>(tx) * XT, j0 = static_cast<int64_t>(ty) * YT;
+    Tile tile;
+    tile.run(a, g, i0, j0, 0, k, steps);
+    const float unit = gradient_unit(TYPE, post, weight_max);
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) {
+        const int64_t j = j0 + Tile::at_y(y);
+        if (j >= piece) continue;
+#pragma unroll
+        for (int m = 0; m < Tile::SX; ++m) {
+            const int64_t i = i0 + Tile::at_x(m);
+            if (i < d) store_four<TYPE>(dw + j * lddw + i, tile.acc[m][y] * unit, static_cast<int>(min<int64_t>(4, d - i)), vector);
+        }
+    }
+}
+
+// ---- host ----------------------------------------------------------------------
+static inline int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+static inline int64_t room(int64_t &at, int64_t bytes)
+{
+    const int64_t here = at;
+    at = up(at + bytes, 256);
+    return here;
+}
+
+// Sizes and places of everything a call passes through its workspace.
+struct ClassPlan {
+    int32_t type, planes, wide;         // wide: bytes of a number in memory
+    int64_t n, c, d, k, dp;             // dp: columns of packed rows
+    bool direct_a, direct_w;
+    int yt;                             // rows of a tile
+    int64_t tiles_x, tiles_y, slots;
+    int64_t piece, pieces, ldg, rows_g, rows_z, splits, per_split;
+    int64_t cls, q, entropy, weight_max, lse, sums, hits, a, w, az, g, partial, bytes;
+};
+
+constexpr int kXT = 256;                 // classes of a tile
+
+// wavefronts along the classes of a tile of yt rows
+static int wave_cols(int yt) { return yt == 256 ? 2 : yt == 64 ? 4 : 8; }
+
+static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &s)
+{
+    if (!p || p->n <= 0 || p->c <= 0 || p->d <= 0 || k < 0 || !p->a || !p->w || p->lda < p->d || p->ldw < p->d) return DQ_ERR_INVALID_ARG;
+    if (p->type != DQ_F32 && p->type != DQ_F16 && p->type != DQ_BF16) return DQ_ERR_INVALID_ARG;
+    s = ClassPlan{};
+    s.type = p->type;
+    s.planes = p->type == DQ_F32 ? 3 : 1;
+    s.wide = p->type == DQ_F32 ? 4 : 2;
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(p->a), pw = reinterpret_cast<uintptr_t>(p->w);
+    if (pa % s.wide || pw % s.wide) return DQ_ERR_INVALID_ARG;
+    constexpr int64_t kMost = 1ll << 30;
+    if (p->n > kMost || p->c > kMost || p->d > (1 << 20) || p->lda > (1 << 22) || p->ldw > (1 << 22)) return DQ_ERR_UNSUPPORTED;
+    if (k > DQ_MAX_TEACHER) return DQ_ERR_UNSUPPORTED;
+    s.n = p->n;
+    s.c = p->c;
+    s.d = p->d;
+    s.k = k ? k : 1;
+    s.dp = up(s.d, 64);
+    s.direct_a = s.planes == 1 && s.d % 32 == 0 && p->lda % 8 == 0 && pa % 16 == 0;
+    s.direct_w = s.planes == 1 && s.d % 32 == 0 && p->ldw % 8 == 0 && pw % 16 == 0;
+    s.yt = s.n <= 16 ? 16 : s.n <= 64 ? 64 : 256;
+    s.tiles_x = (s.c + kXT - 1) / kXT;
+    s.tiles_y = (s.n + s.yt - 1) / s.yt;
+    if (s.tiles_x * s.tiles_y > kMost) return DQ_ERR_UNSUPPORTED;
+    s.slots = s.tiles_x * wave_cols(s.yt);
+    int64_t at = 0;
+    s.cls = room(at, 4 * s.n * s.k);
+    s.q = room(at, k ? 4 * s.n * s.k : 0);
+    s.entropy = room(at, k ? 4 * s.n : 0);
+    s.weight_max = room(at, 4);
+    s.lse = room(at, 4 * s.n);
+    s.sums = room(at, 8 * s.slots * s.n);
+    s.hits = room(at, 4 * s.slots * s.n);
+    s.a = room(at, s.direct_a ? 0 : 2 * s.planes * s.n * s.dp);
+    s.w = room(at, s.direct_w ? 0 : 2 * s.planes * s.c * s.dp);
+    if (grad) {
+        s.rows_z = up(s.n, 64);
+        s.rows_g = s.tiles_y * s.yt;
+        const int64_t most = std::max<int64_t>(kPieceBytes / (2 * s.planes * s.rows_g) / kXT, 1) * kXT;
+        s.pieces = (s.c + most - 1) / most;
+        s.piece = up((s.c + s.pieces - 1) / s.pieces, kXT);
+        s.pieces = (s.c + s.piece - 1) / s.piece;
+        s.ldg = s.piece;
+        // da has few tiles: its classes are split until the chip is full, though not below eight stages each
+        const int64_t tiles = (s.d + kXT - 1) / kXT * s.tiles_y;
+        s.splits = std::clamp<int64_t>(512 / tiles, 1, std::max<int64_t>(s.piece / 512, 1));
+        s.per_split = up((s.piece + s.splits - 1) / s.splits, 64);
+        s.splits = (s.piece + s.per_split - 1) / s.per_split;
+        s.az = room(at, 2 * s.planes * s.rows_z * s.dp);
+        s.g = room(at, 2 * s.planes * s.rows_g * s.ldg);
+        s.partial = room(at, 4 * s.splits * s.n * s.dp);
+    }
+    s.bytes = up(at, 16);
+    return DQ_OK;
+}
+
+template <int TYPE>
+static int32_t pack_rows(const void *v, int64_t ld, int64_t rows, int64_t cols, char *out, int64_t out_cols, int64_t out_rows, const int32_t *cls,
+                         int64_t k, hipStream_t st)
+{
+    const int64_t blocks = std::min<int64_t>((out_rows * out_cols / 8 + 255) / 256, 1 << 16);
+    pack_rows_kernel<TYPE><<<static_cast<unsigned>(blocks), 256, 0, st>>>(static_cast<const typename Num<TYPE>::Mem *>(v), ld, rows, cols,
+                                                                          reinterpret_cast<u16 *>(out), out_cols, out_rows, cls, k);
+    DQ_LAUNCH_CHECK();
+    return DQ_OK;
+}
+
+struct ClassCall {
+    const dq_classes *prob;
+    const int32_t *label;
+    const dq_teacher *teacher;
+    const float *weight;
+    float scale;
+    float *loss, *lse;
+    void *da;
+    int64_t ldda;
+    void *dw;
+    int64_t lddw;
+    bool grad;
+    uint32_t *status;
+    char *ws;
+    hipStream_t st;
+};
+
+template <int TYPE, int YT, int WX, int WY>
+static int32_t class_run(const ClassCall &q, const ClassPlan &s)
+{
+    const dq_classes &p = *q.prob;
+    char *const ws = q.ws;
+    const hipStream_t st = q.st;
+    const int64_t n = s.n, c = s.c, wide = s.wide;
+    const int steps = s.planes == 3 ? kPartSteps : 1;
+    const unsigned threads = WX * WY * kWave;
+    int32_t *const cls = reinterpret_cast<int32_t *>(ws + s.cls);
+    const float tau = q.teacher ? q.teacher->tau : 1.0f;
+    Targets targets{cls, nullptr, static_cast<int32_t>(s.k)};
+    const float *entropy = nullptr;
+    if (q.teacher) {
+        int pow2 = 1;
+        while (pow2 < s.k) pow2 *= 2;
+        float *const tq = reinterpret_cast<float *>(ws + s.q), *const ent = reinterpret_cast<float *>(ws + s.entropy);
+        teacher_kernel<<<static_cast<unsigned>(n), kTeacherThreads, 0, st>>>(q.teacher->cls, q.teacher->logit, q.teacher->ld, targets.k, pow2, c,
+                                                                             1.0f / tau, cls, tq, ent, q.status);
+        targets.q = tq;
+        entropy = ent;
+    } else {
+        label_kernel<<<static_cast<unsigned>((n + 255) / 256), 256, 0, st>>>(q.label, n, c, cls, q.status);
+    }
+    DQ_LAUNCH_CHECK();
+
+    // operands: in place, or packed
+    Operand a{static_cast<const char *>(p.a), p.lda * 2, n, 0, 0}, w{static_cast<const char *>(p.w), p.ldw * 2, c, static_cast<int32_t>(s.d), 0};
+    if (!s.direct_a) {
+        if (const int32_t e = pack_rows<TYPE>(p.a, p.lda, n, s.d, ws + s.a, s.dp, n, nullptr, 0, st)) return e;
+        a = Operand{ws + s.a, s.dp * 2, n, 0, n * s.dp * 2};
+    }
+    if (!s.direct_w) {
+        if (const int32_t e = pack_rows<TYPE>(p.w, p.ldw, c, s.d, ws + s.w, s.dp, c, nullptr, 0, st)) return e;
+        w = Operand{ws + s.w, s.dp * 2, c, static_cast<int32_t>(s.dp), c * s.dp * 2};
+    }
+    const int64_t kd = up(s.d, 32);
+    float2 *const sums = reinterpret_cast<float2 *>(ws + s.sums);
+    float *const hits = reinterpret_cast<float *>(ws + s.hits), *const lse = reinterpret_cast<float *>(ws + s.lse);
+    scores_kernel<TYPE, kXT, YT, WX, WY><<<static_cast<unsigned>(s.tiles_x * s.tiles_y), threads, 0, st>>>(
+        w, a, kd, steps, n, c, 1.0f / tau, targets, static_cast<int>(s.tiles_x), static_cast<int>(s.tiles_y), sums, hits);
+    DQ_LAUNCH_CHECK();
+    finish_kernel<<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(sums, hits, static_cast<int>(s.slots), n, cls, targets.k, entropy, tau * tau,
+                                                                        q.loss, q.lse, q.grad ? lse : nullptr, q.status);
+    DQ_LAUNCH_CHECK();
+    if (!q.grad || !(q.da || q.dw)) return DQ_OK;
+
+    const float post = q.scale * tau;
+    float *weight_max = nullptr;
+    if (TYPE == DQ_F16 && q.weight) {
+        weight_max = reinterpret_cast<float *>(ws + s.weight_max);
+        weight_max_kernel<<<1, 1024, 0, st>>>(q.weight, n, weight_max);
+        DQ_LAUNCH_CHECK();
+    }
+    Operand az{ws + s.az, s.dp * 2, s.rows_z, static_cast<int32_t>(s.dp), s.rows_z * s.dp * 2};
+    if (q.dw)
+        if (const int32_t e = pack_rows<TYPE>(p.a, p.lda, n, s.d, ws + s.az, s.dp, s.rows_z, cls, s.k, st)) return e;
+    u16 *const g = reinterpret_cast<u16 *>(ws + s.g);
+    float *const partial = reinterpret_cast<float *>(ws + s.partial);
+    const int64_t plane = s.rows_g * s.ldg;
+    const int tiles_d = static_cast<int>((s.d + kXT - 1) / kXT);
+    typedef typename Num<TYPE>::Mem Mem;
+    for (int64_t at = 0; at < c; at += s.piece) {
+        const int64_t have = std::min(s.piece, c - at);
+        const int tiles_p = static_cast<int>((have + kXT - 1) / kXT);
+        grad_kernel<TYPE, kXT, YT, WX, WY><<<static_cast<unsigned>(tiles_p * s.tiles_y), threads, 0, st>>>(
+            w, a, kd, steps, n, c, at, have, 1.0f / tau, targets, lse, q.weight, weight_max, tiles_p, static_cast<int>(s.tiles_y), g, s.ldg, plane);
+        DQ_LAUNCH_CHECK();
+        const Operand along{reinterpret_cast<const char *>(g), s.ldg * 2, s.rows_g, 0, plane * 2};
+        if (q.da) {
+            const Operand piece{w.p + at * w.ld, w.ld, c - at, w.cols, w.plane};
+            da_kernel<TYPE, kXT, YT, WX, WY><<<dim3(static_cast<unsigned>(tiles_d * s.tiles_y), static_cast<unsigned>(s.splits)), threads, 0, st>>>(
+                piece, along, up(have, 64), s.per_split, steps, n, tiles_d, static_cast<int>(s.tiles_y), partial, s.dp, at == 0);
+            DQ_LAUNCH_CHECK();
+        }
+        if (q.dw) {
+            const Operand across{reinterpret_cast<const char *>(g), s.ldg * 2, s.rows_g, static_cast<int32_t>(s.ldg), plane * 2};
+            dw_kernel<TYPE, kXT, 256, 2, 4><<<static_cast<unsigned>(tiles_d * tiles_p), 512, 0, st>>>(
+                az, across, up(n, 32), steps, have, s.d, tiles_d, tiles_p, post, weight_max, static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw,
+                four_at_once(q.dw, q.lddw, static_cast<int>(wide)));
+            DQ_LAUNCH_CHECK();
+        }
+    }
+    if (q.da) {
+        const int64_t blocks = std::min<int64_t>((n * ((s.d + 3) / 4) + 255) / 256, 1 << 16);
+        da_finish_kernel<TYPE><<<static_cast<unsigned>(blocks), 256, 0, st>>>(partial, static_cast<int>(s.splits), n, s.d, s.dp, cls, targets.k, post,
+                                                                              weight_max, static_cast<Mem *>(q.da), q.ldda,
+                                                                              four_at_once(q.da, q.ldda, static_cast<int>(wide)));
+        DQ_LAUNCH_CHECK();
+    }
+    return DQ_OK;
+}
+
+template <int TYPE>
+static int32_t class_run_type(const ClassCall &q, const ClassPlan &s)
+{
+    switch (s.yt) {
+    case 16: return class_run<TYPE, 16, 8, 1>(q, s);
+    case 64: return class_run<TYPE, 64, 4, 2>(q, s);
+    default: return class_run<TYPE, 256, 2, 4>(q, s);
+    }
+}
+
+static int32_t class_call(ClassCall &q, void *ws, int64_t ws_bytes)
+{
+    ClassPlan s;
+    const int64_t k = q.teacher ? q.teacher->k : 0;
+    if (q.teacher && (k <= 0 || !q.teacher->cls || !q.teacher->logit || q.teacher->ld < k || !(q.teacher->tau > 0.0f) ||
+                      !__builtin_isfinite(q.teacher->tau)))
+        return DQ_ERR_INVALID_ARG;
+    if (!q.teacher && !q.label) return DQ_ERR_INVALID_ARG;
+    if (const int32_t e = class_plan(q.prob, k, q.grad, s)) return e;
+    const int32_t wide = s.wide;
+    if ((q.da && (q.ldda < s.d || reinterpret_cast<uintptr_t>(q.da) % wide)) || (q.dw && (q.lddw < s.d || reinterpret_cast<uintptr_t>(q.dw) % wide)))
+        return DQ_ERR_INVALID_ARG;
+    if (!ws || !aligned16(ws)) return DQ_ERR_INVALID_ARG;
+    if (ws_bytes < s.bytes) return DQ_ERR_WORKSPACE;
+    q.ws = static_cast<char *>(ws);
+    switch (s.type) {
+    case DQ_F32: return class_run_type<DQ_F32>(q, s);
+    case DQ_F16: return class_run_type<DQ_F16>(q, s);
+    default: return class_run_type<DQ_BF16>(q, s);
+    }
+}
+
+}  // namespace dq
+
+extern "C" int64_t dq_class_workspace_bytes(int32_t op, const dq_classes *prob, int64_t k)
+{
+    if (op != DQ_OP_CLASS_LOSS && op != DQ_OP_CLASS_GRAD) return DQ_ERR_INVALID_ARG;
+    dq::ClassPlan s;
+    const int32_t e = dq::class_plan(prob, k, op == DQ_OP_CLASS_GRAD, s);
+    return e ? e : s.bytes;
+}
+
+extern "C" int32_t dq_class_loss(const dq_classes *prob, const int32_t *label, float *loss_out, float *lse_out, uint32_t *status, void *ws,
+                                 int64_t ws_bytes, void *stream)
+{
+    if (!loss_out) return DQ_ERR_INVALID_ARG;
+    dq::ClassCall q{prob, label, nullptr, nullptr, 1.0f, loss_out, lse_out, nullptr, 0, nullptr, 0, false, status, nullptr, static_cast<hipStream_t>(stream)};
+    return dq::class_call(q, ws, ws_bytes);
+}
+
+extern "C" int32_t dq_class_grad(const dq_classes *prob, const int32_t *label, const float *weight, float scale, float *loss_out, float *lse_out,
+                                 void *da_out, int64_t ldda, void *dw_out, int64_t lddw, uint32_t *status, void *ws, int64_t ws_bytes, void *stream)
+{
+    dq::ClassCall q{prob, label, nullptr, weight, scale, loss_out, lse_out, da_out, ldda, dw_out, lddw, true, status, nullptr, static_cast<hipStream_t>(stream)};
+    return dq::class_call(q, ws, ws_bytes);
+}
+
+extern "C" int32_t dq_distill_loss(const dq_classes *prob, const dq_teacher *teacher, float *loss_out, float *lse_out, uint32_t *status, void *ws,
+                                   int64_t ws_bytes, void *stream)
+{
+    if (!loss_out || !teacher) return DQ_ERR_INVALID_ARG;
+    dq::ClassCall q{prob, nullptr, teacher, nullptr, 1.0f, loss_out, lse_out, nullptr, 0, nullptr, 0, false, status, nullptr, static_cast<hipStream_t>(stream)};
+    return dq::class_call(q, ws, ws_bytes);
+}
+
+extern "C" int32_t dq_distill_grad(const dq_classes *prob, const dq_teacher *teacher, const float *weight, float scale, float *loss_out,
+                                   float *lse_out, void *da_out, int64_t ldda, void *dw_out, int64_t lddw, uint32_t *status, void *ws, int64_t ws_bytes,
+                                   void *stream)
+{
+    if (!teacher) return DQ_ERR_INVALID_ARG;
+    dq::ClassCall q{prob, nullptr, teacher, weight, scale, loss_out, lse_out, da_out, ldda, dw_out, lddw, true, status, nullptr, static_cast<hipStream_t>(stream)};
+    return dq::class_call(q, ws, ws_bytes);
+}
