@@ -177,7 +177,7 @@ __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp
 
 // Sums of a tile's row are kept per wavefront column (slot): the row's maximum, the sum of exp above it, the targets' sum q z.
 template <int TYPE, int XT, int YT, int WX, int WY>
-__global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operand a, int64_t k, int steps, int64_t n, int64_t c,
+__global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c,
                                                                float inv_tau, Targets targets, int tiles_x, int tiles_y,
                                                                float2 *__restrict__ sums, float *__restrict__ hits)
 {
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operan
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t c0 = static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
     Tile tile;
-    tile.run(w, a, c0, t0, 0, k, steps);
+    tile.template run<TYPE == DQ_F32>(w, a, c0, t0, 0, k);
     const int lane = threadIdx.x & 63, wave_c0 = static_cast<int>(c0) + Tile::sub_x(0) * 16;
     const int64_t slot = static_cast<int64_t>(tx) * WX + Tile::wave() % WX;
 #pragma unroll
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2 *__restrict__ 
 // ---- gradients -----------------------------------------------------------------
 // g of a piece of the classes, [rows of the tiles][ldg] in 16 bits (three planes for float32); zeros where there is no row or class.
 template <int TYPE, int XT, int YT, int WX, int WY>
-__global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand a, int64_t k, int steps, int64_t n, int64_t c, int64_t piece0,
+__global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, int64_t piece0,
                                                              int64_t piece, float inv_tau, Targets targets, const float *__restrict__ lse,
                                                              const float *__restrict__ weight, const float *__restrict__ weight_max,
                                                              int tiles_x, int tiles_y, u16 *__restrict__ g, int64_t ldg, int64_t plane)
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand 
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t c0 = piece0 + static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
     Tile tile;
-    tile.run(w, a, c0, t0, 0, k, steps);
+    tile.template run<TYPE == DQ_F32>(w, a, c0, t0, 0, k);
     const int wave_c0 = static_cast<int>(c0) + Tile::sub_x(0) * 16;
 #pragma unroll
     for (int y = 0; y < Tile::SY; ++y) {
@@ -346,17 +346,17 @@ __device__ __forceinline__ float gradient_unit(int type, float post, const float
 
 // da of a piece, one split of its classes per blockIdx.y: partial sums [split][n][ldp] in float32, added to what the pieces before left.
 template <int TYPE, int XT, int YT, int WX, int WY>
-__global__ __launch_bounds__(WX *WY *kWave) void da_kernel(Operand w, Operand g, int64_t piece, int64_t per_split, int steps, int64_t n, int tiles_x,
+__global__ __launch_bounds__(WX *WY *kWave) void da_kernel(Operand w, Operand g, int64_t piece, int64_t per_split, int64_t n, int tiles_x,
                                                            int tiles_y, float *__restrict__ partial, int64_t ldp, int first)
 {
     typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, false> Tile;
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t i0 = static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT, k0 = blockIdx.y * per_split;
-    const int64_t k1 = min(k0 + per_split, piece);
+    const int64_t k1 = lesser(k0 + per_split, piece);
     if (k0 >= k1 && !first) return;
     Tile tile;
-    tile.run(w, g, i0, t0, k0, max(k0, k1), steps);
+    tile.template run<TYPE == DQ_F32>(w, g, i0, t0, k0, k0 < k1 ? k1 : k0);
     float *const out = partial + blockIdx.y * n * ldp;
 #pragma unroll
     for (int y = 0; y < Tile::SY; ++y) {
@@ -387,12 +387,12 @@ __global__ __launch_bounds__(256) void da_finish_kernel(const float *__restrict_
             for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x4 *>(partial + (s * n + t) * ldp + i);
             v *= unit;
         }
-        store_four<TYPE>(da + t * ldda + i, v, static_cast<int>(min<int64_t>(4, d - i)), vector);
+        store_four<TYPE>(da + t * ldda + i, v, static_cast<int>(lesser(4, d - i)), vector);
     }
 }
 
 template <int TYPE, int XT, int YT, int WX, int WY>
-__global__ __launch_bounds__(WX *WY *kWave) void dw_kernel(Operand a, Operand g, int64_t k, int steps, int64_t piece, int64_t d, int tiles_x, int tiles_y,
+__global__ __launch_bounds__(WX *WY *kWave) void dw_kernel(Operand a, Operand g, int64_t k, int64_t piece, int64_t d, int tiles_x, int tiles_y,
                                                            float post, const float *__restrict__ weight_max,
                                                            typename Num<TYPE>::Mem *__restrict__ dw, int64_t lddw, int vector)
 {
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void dw_kernel(Operand a, Operand g,
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t i0 = static_cast<int64_t>(tx) * XT, j0 = static_cast<int64_t>(ty) * YT;
     Tile tile;
-    tile.run(a, g, i0, j0, 0, k, steps);
+    tile.template run<TYPE == DQ_F32>(a, g, i0, j0, 0, k);
     const float unit = gradient_unit(TYPE, post, weight_max);
 #pragma unroll
     for (int y = 0; y < Tile::SY; ++y) {
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void dw_kernel(Operand a, Operand g,
 #pragma unroll
         for (int m = 0; m < Tile::SX; ++m) {
             const int64_t i = i0 + Tile::at_x(m);
-            if (i < d) store_four<TYPE>(dw + j * lddw + i, tile.acc[m][y] * unit, static_cast<int>(min<int64_t>(4, d - i)), vector);
+            if (i < d) store_four<TYPE>(dw + j * lddw + i, tile.acc[m][y] * unit, static_cast<int>(lesser(4, d - i)), vector);
         }
     }
 }
@@ -531,7 +531,6 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     char *const ws = q.ws;
     const hipStream_t st = q.st;
     const int64_t n = s.n, c = s.c, wide = s.wide;
-    const int steps = s.planes == 3 ? kPartSteps : 1;
     const unsigned threads = WX * WY * kWave;
     int32_t *const cls = reinterpret_cast<int32_t *>(ws + s.cls);
     const float tau = q.teacher ? q.teacher->tau : 1.0f;
@@ -564,7 +563,7 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     float2 *const sums = reinterpret_cast<float2 *>(ws + s.sums);
     float *const hits = reinterpret_cast<float *>(ws + s.hits), *const lse = reinterpret_cast<float *>(ws + s.lse);
     scores_kernel<TYPE, kXT, YT, WX, WY><<<static_cast<unsigned>(s.tiles_x * s.tiles_y), threads, 0, st>>>(
-        w, a, kd, steps, n, c, 1.0f / tau, targets, static_cast<int>(s.tiles_x), static_cast<int>(s.tiles_y), sums, hits);
+        w, a, kd, n, c, 1.0f / tau, targets, static_cast<int>(s.tiles_x), static_cast<int>(s.tiles_y), sums, hits);
     DQ_LAUNCH_CHECK();
     finish_kernel<<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(sums, hits, static_cast<int>(s.slots), n, cls, targets.k, entropy, tau * tau,
                                                                         q.loss, q.lse, q.grad ? lse : nullptr, q.status);
@@ -590,19 +589,19 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
         const int64_t have = std::min(s.piece, c - at);
         const int tiles_p = static_cast<int>((have + kXT - 1) / kXT);
         grad_kernel<TYPE, kXT, YT, WX, WY><<<static_cast<unsigned>(tiles_p * s.tiles_y), threads, 0, st>>>(
-            w, a, kd, steps, n, c, at, have, 1.0f / tau, targets, lse, q.weight, weight_max, tiles_p, static_cast<int>(s.tiles_y), g, s.ldg, plane);
+            w, a, kd, n, c, at, have, 1.0f / tau, targets, lse, q.weight, weight_max, tiles_p, static_cast<int>(s.tiles_y), g, s.ldg, plane);
         DQ_LAUNCH_CHECK();
         const Operand along{reinterpret_cast<const char *>(g), s.ldg * 2, s.rows_g, 0, plane * 2};
         if (q.da) {
             const Operand piece{w.p + at * w.ld, w.ld, c - at, w.cols, w.plane};
             da_kernel<TYPE, kXT, YT, WX, WY><<<dim3(static_cast<unsigned>(tiles_d * s.tiles_y), static_cast<unsigned>(s.splits)), threads, 0, st>>>(
-                piece, along, up(have, 64), s.per_split, steps, n, tiles_d, static_cast<int>(s.tiles_y), partial, s.dp, at == 0);
+                piece, along, up(have, 64), s.per_split, n, tiles_d, static_cast<int>(s.tiles_y), partial, s.dp, at == 0);
             DQ_LAUNCH_CHECK();
         }
         if (q.dw) {
             const Operand across{reinterpret_cast<const char *>(g), s.ldg * 2, s.rows_g, static_cast<int32_t>(s.ldg), plane * 2};
             dw_kernel<TYPE, kXT, 256, 2, 4><<<static_cast<unsigned>(tiles_d * tiles_p), 512, 0, st>>>(
-                az, across, up(n, 32), steps, have, s.d, tiles_d, tiles_p, post, weight_max, static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw,
+                az, across, up(n, 32), have, s.d, tiles_d, tiles_p, post, weight_max, static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw,
                 four_at_once(q.dw, q.lddw, static_cast<int>(wide)));
             DQ_LAUNCH_CHECK();
         }

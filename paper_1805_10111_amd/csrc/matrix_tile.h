@@ -7,8 +7,8 @@
 //
 // Either operand is stored along k (row-major rows i, k contiguous), or across it (row-major rows k, i contiguous); the latter
 // reaches the matrix cores through the transposing reads of LDS, so nothing is ever transposed in memory.
-// A stage is 128 bytes of k: 64 numbers of 16 bits, 256 of 4.  Two stages of both operands lie in LDS, filled by loads that go there
-// directly; while one is multiplied the other is on its way.
+// A stage is 64 bytes of k: 32 numbers of 16 bits, 128 of 4.  LDS holds a ring of four, filled by loads that go there directly: while
+// one is multiplied, three are on their way.
 //
 // What bounds it: the matrix cores.  256 x 256 with eight wavefronts (a wavefront multiplies 128 x 64: 12 reads of LDS for 32
 // products) needs 96 KB of LDS reads per 1024 cycles of matrix-core work, and each byte of memory is used for 256 products.
@@ -29,16 +29,17 @@ typedef __attribute__((ext_vector_type(8))) short i16x8;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 
-constexpr int kStageBytes = 128;               // of k, per row of an operand stored along k
-constexpr int kStageRows = 64;                 // of k, for an operand stored across it (16-bit numbers)
+constexpr int kStageBytes = 64;                // of k, per row of an operand stored along k
+constexpr int kStageRows = 32;                 // of k, for an operand stored across it (16-bit numbers)
+constexpr int kRing = 4;                       // stages in LDS
 
-// An operand in memory.  Its row i (row k where it is stored across k) begins at p + i * ld bytes; rows is how many there are:
-// reads past the last are turned to the last, whose products the caller drops (i) or meets with zeros of the other operand (k).
+// An operand in memory.  Its row i (row k where it is stored across k) begins at p + i * ld bytes; rows is how many there are.
+// Nothing outside of it is read: rows past the last are zeros, and k past its end.
 struct Operand {
     const char *p;
     int64_t ld;            // bytes, a multiple of 16
     int64_t rows;
-    int32_t cols;          // stored across k: how many i there are (a multiple of 8); unused otherwise
+    int32_t cols;          // stored across k: how many i there are; unused otherwise
     int64_t plane;         // bytes from one part of a number to the next (float32 as three bfloat16), 0 otherwise
     const uint8_t *scales; // 4-bit numbers: four scales per 64 bytes of a row, from row to row ld_scales bytes
     int64_t ld_scales;
@@ -65,95 +66,132 @@ struct MulF16 {
     }
 };
 
-// 128 numbers of 4 bits: a lane holds 32 of them, one block, and the low byte of sx, sy is that block's scale.
+// 128 numbers of 4 bits: a lane holds 32 of them, one block; byte m of sx, n of sy is that block's scale.
 struct MulMx4 {
     static constexpr bool kScaled = true;
-    static __device__ __forceinline__ f32x4 mul(i32x4 x, i32x4 y, f32x4 c, uint32_t sx, uint32_t sy)
+    static __device__ __forceinline__ f32x4 mul(i32x4 x, i32x4 y, f32x4 c, int sx, int m, int sy, int n)
     {
         const i32x8 a{x[0], x[1], x[2], x[3], 0, 0, 0, 0}, b{y[0], y[1], y[2], y[3], 0, 0, 0, 0};
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, 0, static_cast<int>(sx), 0, static_cast<int>(sy));
+#define DQ_MX4(M, N) case M * 4 + N: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, M, sx, N, sy)
+        switch (m * 4 + n) {                   // (which byte is part of the instruction: m and n are known when it is compiled)
+            DQ_MX4(0, 0); DQ_MX4(0, 1); DQ_MX4(0, 2); DQ_MX4(0, 3); DQ_MX4(1, 0); DQ_MX4(1, 1); DQ_MX4(1, 2); DQ_MX4(1, 3);
+            DQ_MX4(2, 0); DQ_MX4(2, 1); DQ_MX4(2, 2); DQ_MX4(2, 3); DQ_MX4(3, 0); DQ_MX4(3, 1); DQ_MX4(3, 2); DQ_MX4(3, 3);
+        }
+#undef DQ_MX4
+        return c;
     }
 };
 
-typedef const __attribute__((address_space(1))) void *GlobalPtr;
 typedef __attribute__((address_space(3))) void *LdsPtr;
 typedef __attribute__((address_space(3))) i16x4 *LdsQuad;
 
-__device__ __forceinline__ void load_to_lds(const char *from, char *to)
-{
-    __builtin_amdgcn_global_load_lds((GlobalPtr)from, (LdsPtr)to, 16, 0, 0);
-}
+__device__ __forceinline__ int64_t lesser(int64_t a, int64_t b) { return a < b ? a : b; }      // (min() goes through doubles)
 
-// The stage that is on its way has arrived, in every wavefront, and every wavefront is done with the one before.
+// All but the newest NEWER loads of this wavefront have arrived, in every wavefront, and every wavefront has read what it wanted of
+// LDS.  (__syncthreads() would wait for all loads.)
+template <int NEWER>
 __device__ __forceinline__ void stage_arrived()
 {
-    __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
-    __syncthreads();
+    static_assert(NEWER < 64, "six bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (NEWER & 15) | (NEWER >> 4) << 14);      // vmcnt(NEWER), lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 // The loads of one operand's stages.  ACROSS: stored across k.
 // LDS holds a stage as it lies in memory, its 16-byte chunks permuted within a row so that no two of the lanes that read together
-// meet a bank: along k, chunk c of row r at c ^ (r / 2) % 8 (16 lanes read 16 rows of 128 bytes); across k, 32 bytes at a time,
+// meet a bank: along k, chunk c of row r at c ^ (r / 4) % 4 (16 lanes read 16 rows of 64 bytes); across k, 32 bytes at a time,
 // pair c of row k at c ^ (k % 4 + 4 (k / 8 % 2)) (32 lanes read rows k .. k + 3 and k + 8 .. k + 11).
 template <int T, bool ACROSS, int THREADS>
 struct StageLoads {
-    static constexpr int kChunks = (T * 8 + THREADS - 1) / THREADS;
-    static constexpr int kRowChunks = ACROSS ? T / 8 : 8;
+    static constexpr int kChunks = (T * 4 + THREADS - 1) / THREADS;              // loads of a thread per stage
+    static constexpr int kSurely = T * 4 / THREADS;                              // ... of any thread
+    static constexpr int kRowChunks = ACROSS ? T / 8 : 4;
     static constexpr int kPairMask = T / 16 >= 8 ? 7 : T / 16 - 1;
     uint32_t off[kChunks];
-    int64_t ld;
 
-    __device__ __forceinline__ void init(const Operand &o, int64_t i0)
+    __device__ __forceinline__ void init(const Operand &o)
     {
-        ld = o.ld;
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
             const int id = threadIdx.x + i * THREADS, row = id / kRowChunks, slot = id % kRowChunks;
-            if constexpr (ACROSS) {
-                const int pair = (slot >> 1) ^ (((row & 3) | ((row >> 1) & 4)) & kPairMask);
-                const int col = min(static_cast<int>(i0) + (pair * 2 + (slot & 1)) * 8, o.cols - 8);
-                off[i] = static_cast<uint32_t>(col) * 2u;
-            } else {
-                const int64_t r = i0 + row < o.rows ? row : o.rows - 1 - i0;
-                off[i] = static_cast<uint32_t>(r * o.ld) + static_cast<uint32_t>(slot ^ ((row >> 1) & 7)) * 16u;
-            }
+            int at;
+            if constexpr (ACROSS) at = (((slot >> 1) ^ (((row & 3) | ((row >> 1) & 4)) & kPairMask)) * 2 + (slot & 1)) * 16;
+            else at = (slot ^ ((row >> 2) & 3)) * 16;
+            off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(o.ld) + static_cast<uint32_t>(at);
         }
     }
-    // base: where the stage's k begins (row k0, or byte k0 of row i0).  left: how much of k there is from there on (rows, or bytes; a
-    // multiple of 64 bytes).
-    __device__ __forceinline__ void issue(const char *base, int64_t left, char *lds) const
+    // `part` of `parts` of the loads; to: where this wavefront's first one goes.
+    __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t from, char *ring, int to, int part, int parts) const
     {
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
-            const int id = threadIdx.x + i * THREADS, first = id & ~(kWave - 1);
-            if (kChunks * THREADS > T * 8 && first >= T * 8) break;
-            uint32_t at = off[i];
-            if constexpr (ACROSS) {
-                const int row = id / kRowChunks;
-                at += static_cast<uint32_t>(left < kStageRows ? min(row, static_cast<int>(left) - 1) : row) * static_cast<uint32_t>(ld);
-            } else if (left < kStageBytes) {
-                const int row = id / 8, chunk = (id % 8) ^ ((row >> 1) & 7);
-                at -= static_cast<uint32_t>(chunk & 4) * 16u;
-            }
-            load_to_lds(base + at, lds + first * 16);
+            if (i * parts / kChunks != part) continue;
+            if (kChunks != kSurely && static_cast<int>(threadIdx.x) + i * THREADS >= T * 4) continue;      // (whole wavefronts)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (LdsPtr)(ring + (to + i * THREADS * 16)), 16, static_cast<int>(off[i]), 0, 0, 0);
         }
     }
 };
 
-// What a lane reads from a stage for subtile `sub` and 32 numbers of k.
+// Where an operand's next stage lies: a buffer, behind whose end everything reads as zero.  (Loads to LDS go through buffers also
+// because the compiler takes those through plain pointers for possible accesses to LDS by address, and then waits for all reads of
+// LDS at every use of one.)  Moving on takes a few scalar instructions.
 template <int T, bool ACROSS>
-__device__ __forceinline__ i32x4 stage_part(const char *lds, int sub, int half)
+struct Reader {
+    const char *p;
+    int32_t left;                        // across k: rows from here on; along k: bytes from here to the end of the tile's last row
+    int32_t ld, edge;                    // across k: bytes of a row, and by how much the last one is shorter
+    __device__ __forceinline__ Reader(const Operand &o, int64_t i0, int64_t k0, int64_t k1)
+    {
+        ld = static_cast<int32_t>(o.ld);
+        if constexpr (ACROSS) {
+            p = o.p + k0 * o.ld + i0 * 2;
+            left = static_cast<int32_t>(o.rows - k0);
+            edge = static_cast<int32_t>(2 * (o.cols - i0) - o.ld);
+        } else {
+            p = o.p + i0 * o.ld + k0 * 2;
+            left = static_cast<int32_t>((lesser(o.rows - i0, T) - 1) * o.ld + 2 * (k1 - k0));
+            edge = 0;
+        }
+    }
+    // any: whether there is another stage
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(bool any) const
+    {
+        const int32_t bytes = ACROSS ? max(min(left, kStageRows) * ld + edge, 0) : left;
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p), 0, any ? bytes : 0, 0x00027000);
+    }
+    __device__ __forceinline__ void next()
+    {
+        p += ACROSS ? static_cast<int64_t>(kStageRows) * ld : kStageBytes;
+        left -= ACROSS ? kStageRows : kStageBytes;
+    }
+};
+
+// Where in an operand's part of a stage a lane reads of subtile 0 of those of its wavefront (subtiles first ..).
+template <int T, bool ACROSS>
+__device__ __forceinline__ int part_address(int first)
 {
     const int lane = threadIdx.x & (kWave - 1), j = lane & 15, g = lane >> 4;
     if constexpr (ACROSS) {
         constexpr int mask = T / 16 >= 8 ? 7 : T / 16 - 1;
-        const int f = ((j >> 2) | ((g & 1) << 2)) & mask;
-        const char *at = lds + (half * 32 + g * 8 + (j >> 2)) * (T * 2) + ((sub ^ f) * 32) + (j & 3) * 8;
-        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)at);
-        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(at + 4 * T * 2));
+        return (g * 8 + (j >> 2)) * (T * 2) + ((first ^ (((j >> 2) | ((g & 1) << 2)) & mask)) * 32) + (j & 3) * 8;
+    } else {
+        return (first * 16 + j) * kStageBytes + ((g ^ (j >> 2)) * 16);
+    }
+}
+// ... and what it reads of subtile m of them (there are a power of two of them, their first a multiple of it).  An operand's part of the
+// ring begins `from` in.  (One addition to the array: the compiler follows an address to its array through a few additions only.)
+template <int T, bool ACROSS>
+__device__ __forceinline__ i32x4 stage_part(const char *ring, int from, int address, int m)
+{
+    if constexpr (ACROSS) {
+        const int at = address ^ (m * 32);
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(ring + (from + at)));
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(ring + (from + 4 * T * 2 + at)));
         return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-        return *reinterpret_cast<const i32x4 *>(lds + (sub * 16 + j) * kStageBytes + (((half * 4 + g) ^ (j >> 1)) * 16));
+        return *reinterpret_cast<const i32x4 *>(ring + (from + m * 16 * kStageBytes + address));
     }
 }
 
@@ -163,6 +201,7 @@ struct TileProduct {
     static constexpr int kThreads = WX * WY * kWave;
     static constexpr int SX = XT / 16 / WX, SY = YT / 16 / WY;
     f32x4 acc[SX][SY];
+    int address_x, address_y;
 
     static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
     static __device__ __forceinline__ int sub_x(int m) { return (wave() % WX) * SX + m; }
@@ -171,92 +210,190 @@ struct TileProduct {
     static __device__ __forceinline__ int at_x(int m) { return sub_x(m) * 16 + ((threadIdx.x & 63) >> 4) * 4; }
     static __device__ __forceinline__ int at_y(int n) { return sub_y(n) * 16 + (threadIdx.x & 15); }
 
-    // The scales of a stage's blocks: of both halves, a lane's own block's in the low byte.
+    // Scales of 4-bit numbers.  A stage has four blocks a row; LDS holds their scales as [block][row % 16][row / 16], so that what a
+    // lane needs for its subtiles are neighbouring bytes.  Thread r brings those of row r (x's rows, then y's).
+    static constexpr int kScaleBytes = 4 * (XT + YT);
+    static_assert(!Mul::kScaled || XT + YT <= kThreads, "a thread brings one row's scales");
     struct Scales {
-        uint32_t x[2][Mul::kScaled ? SX : 1], y[2][Mul::kScaled ? SY : 1];
+        uint32_t x[(SX + 3) / 4], y[(SY + 3) / 4];
     };
-    template <int S>
-    static __device__ __forceinline__ void load_scales(const Operand &o, int64_t row0, int64_t group, int64_t groups, uint32_t (&out)[2][S])
+    template <int S, int T>
+    static __device__ __forceinline__ void read_scales(const uint8_t *lds, int sub, uint32_t (&out)[(S + 3) / 4])
     {
+        const int lane = threadIdx.x & 63;
+        const uint8_t *const at = lds + (lane >> 4) * T + (lane & 15) * (T / 16) + sub;
 #pragma unroll
-        for (int m = 0; m < S; ++m) {
-            const uint8_t *const row = o.scales + min(row0 + m * 16 + (threadIdx.x & 15), o.rows - 1) * o.ld_scales;
-            out[0][m] = *reinterpret_cast<const uint32_t *>(row + group * 4);
-            out[1][m] = *reinterpret_cast<const uint32_t *>(row + min(group + 1, groups - 1) * 4);
-        }
+        for (int i = 0; i < (S + 3) / 4; ++i)
+            out[i] = S >= 4 ? reinterpret_cast<const uint32_t *>(at)[i] : S == 2 ? *reinterpret_cast<const uint16_t *>(at) : *at;
+    }
+    static __device__ __forceinline__ void read_scales(const uint8_t *lds, Scales &s)
+    {
+        read_scales<SX, XT>(lds, sub_x(0), s.x);
+        read_scales<SY, YT>(lds + 4 * XT, sub_y(0), s.y);
+    }
+    static __device__ __forceinline__ uint32_t load_scales(const uint8_t *row, int64_t group, int64_t groups)
+    {
+        return row ? *reinterpret_cast<const uint32_t *>(row + lesser(group, groups - 1) * 4) : 0;
+    }
+    static __device__ __forceinline__ void write_scales(uint8_t *lds, uint32_t v)
+    {
+        const bool in_x = threadIdx.x < XT;
+        const int r = in_x ? threadIdx.x : threadIdx.x - XT, rows = in_x ? XT : YT;
+        if (r >= rows) return;
+        uint8_t *const at = lds + (in_x ? 0 : 4 * XT) + (r & 15) * (rows / 16) + (r >> 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i * rows] = static_cast<uint8_t>(v >> (8 * i));
     }
 
-    __device__ __forceinline__ void multiply(const char *xs, const char *ys, int halves, const Scales &scales)
+    // A stage is multiplied in steps of kQ of x's subtiles; what a step multiplies has been read from LDS a step before.
+    static constexpr int kQ = SX < 4 ? SX : 4, kSteps = SX / kQ;
+    static constexpr int kY = XT * kStageBytes;     // where y's part of a stage begins
+    __device__ __forceinline__ void read_step(const char *ring, int step, i32x4 (&x)[kQ], i32x4 (&y)[SY]) const
     {
-        const int mine = ((threadIdx.x & 63) >> 4) * 8;
+        if (step == 0)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (half && halves < 2) break;
-            i32x4 y[SY];
+            for (int n = 0; n < SY; ++n) y[n] = stage_part<YT, YS>(ring, kY, address_y, n);
 #pragma unroll
-            for (int n = 0; n < SY; ++n) y[n] = stage_part<YT, YS>(ys, sub_y(n), half);
+        for (int m = 0; m < kQ; ++m) x[m] = stage_part<XT, XS>(ring, 0, address_x, step * kQ + m);
+    }
+    __device__ __forceinline__ void multiply_step(const i32x4 (&x)[kQ], const i32x4 (&y)[SY], int step, const Scales &scales)
+    {
 #pragma unroll
-            for (int m = 0; m < SX; ++m) {
-                const i32x4 x = stage_part<XT, XS>(xs, sub_x(m), half);
+        for (int m = 0; m < kQ; ++m)
 #pragma unroll
-                for (int n = 0; n < SY; ++n) {
-                    if constexpr (Mul::kScaled) acc[m][n] = Mul::mul(x, y[n], acc[m][n], scales.x[half][m] >> mine, scales.y[half][n] >> mine);
-                    else acc[m][n] = Mul::mul(x, y[n], acc[m][n]);
-                }
+            for (int n = 0; n < SY; ++n) {
+                f32x4 &c = acc[step * kQ + m][n];
+                const int at = step * kQ + m;
+                if constexpr (Mul::kScaled) c = Mul::mul(x[m], y[n], c, static_cast<int>(scales.x[at / 4]), at % 4, static_cast<int>(scales.y[n / 4]), n % 4);
+                else c = Mul::mul(x[m], y[n], c);
             }
+    }
+    // In what order a step's instructions are issued: the next step's reads of LDS between the first products, so that each has the
+    // rest of the step to arrive (left to itself the compiler puts them right before their use).
+    template <int READS, int PRODUCTS>
+    static __device__ __forceinline__ void order_step()
+    {
+        constexpr int kLds = 0x100, kMatrix = 0x8, kEach = READS > PRODUCTS ? 1 : PRODUCTS / READS > 2 ? 2 : 1;
+#pragma unroll
+        for (int i = 0; i < (READS < PRODUCTS ? READS : PRODUCTS); ++i) {
+            __builtin_amdgcn_sched_group_barrier(kLds, READS > PRODUCTS ? READS / PRODUCTS : 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kMatrix, kEach, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(kMatrix, PRODUCTS, 0);
     }
 
-    // k0 .. k1 (in pairs of bytes, k0 a multiple of 64, k1 of 32) of rows i0.. of x and j0.. of y.  steps: 1, or kPartSteps for parts.
-    __device__ __forceinline__ void run(const Operand &x, const Operand &y, int64_t i0, int64_t j0, int64_t k0, int64_t k1, int steps)
+    // k0 .. k1 (in pairs of bytes, multiples of 32) of rows i0.. of x and j0.. of y.  PARTS: operands are float32 in parts.
+    template <bool PARTS>
+    __device__ __forceinline__ void run(const Operand &x, const Operand &y, int64_t i0, int64_t j0, int64_t k0, int64_t k1)
     {
-        __shared__ __attribute__((aligned(1024))) char xs0[XT * kStageBytes], xs1[XT * kStageBytes];
-        __shared__ __attribute__((aligned(1024))) char ys0[YT * kStageBytes], ys1[YT * kStageBytes];
-        StageLoads<XT, XS, kThreads> lx;
-        StageLoads<YT, YS, kThreads> ly;
-        lx.init(x, i0);
-        ly.init(y, j0);
+        // (an array of its own for each stage: the compiler keeps apart what is read and what is arriving by the array, up to seven)
+        __shared__ __attribute__((aligned(1024))) char ring0[(XT + YT) * kStageBytes], ring1[(XT + YT) * kStageBytes],
+            ring2[(XT + YT) * kStageBytes], ring3[(XT + YT) * kStageBytes];
+        __shared__ __attribute__((aligned(16))) uint8_t scales0[Mul::kScaled ? kScaleBytes : 16], scales1[Mul::kScaled ? kScaleBytes : 16];
+        typedef StageLoads<XT, XS, kThreads> LoadsX;
+        typedef StageLoads<YT, YS, kThreads> LoadsY;
+        LoadsX lx;
+        LoadsY ly;
+        lx.init(x);
+        ly.init(y);
 #pragma unroll
         for (int m = 0; m < SX; ++m)
 #pragma unroll
             for (int n = 0; n < SY; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const char *const px = x.p + (XS ? k0 * x.ld : i0 * x.ld + k0 * 2), *const py = y.p + (YS ? k0 * y.ld : j0 * y.ld + k0 * 2);
-        const int per = static_cast<int>((k1 - k0 + 63) / 64), stages = per * steps;
-        const int64_t dx = XS ? kStageRows * x.ld : kStageBytes, dy = YS ? kStageRows * y.ld : kStageBytes;
-        int at = 0, part = 0;                   // the next stage to be loaded: stage `at` of part product `part`
-        const char *nx = px + (steps > 1 ? (kPartsX & 3) * x.plane : 0), *ny = py + (steps > 1 ? (kPartsY & 3) * y.plane : 0);
-        auto load = [&](char *xs, char *ys, Scales &scales) {
-            const int64_t k = k0 + static_cast<int64_t>(at) * 64;
-            if constexpr (Mul::kScaled) {
-                load_scales(x, i0 + sub_x(0) * 16, k / 32, k1 / 32, scales.x);
-                load_scales(y, j0 + sub_y(0) * 16, k / 32, k1 / 32, scales.y);
-            }
-            lx.issue(nx, XS ? x.rows - k : (k1 - k) * 2, xs);
-            ly.issue(ny, YS ? y.rows - k : (k1 - k) * 2, ys);
-            nx += dx;
-            ny += dy;
-            if (++at == per) {
-                at = 0;
-                ++part;
-                nx = px + ((kPartsX >> (2 * part)) & 3) * x.plane;
-                ny = py + ((kPartsY >> (2 * part)) & 3) * y.plane;
-            }
+        const int per = static_cast<int>((k1 - k0) / 32), stages = PARTS ? per * kPartSteps : per;
+        if (stages <= 0) return;
+        address_x = part_address<XT, XS>(sub_x(0));
+        address_y = part_address<YT, YS>(sub_y(0));
+        const Reader<XT, XS> bx(x, i0, k0, k1);
+        const Reader<YT, YS> by(y, j0, k0, k1);
+        Reader<XT, XS> rx = bx;
+        Reader<YT, YS> ry = by;
+        int coming = stages, at = per, part = 0;     // stages to be loaded yet, of this product of parts
+        auto select = [&] {
+            rx = bx;
+            ry = by;
+            rx.p += ((kPartsX >> (2 * part)) & 3) * x.plane;
+            ry.p += ((kPartsY >> (2 * part)) & 3) * y.plane;
         };
-        const int last = (k1 - k0) % 64 ? 1 : 2;      // halves of the last stage of a part product
-        int done = 0;
-        auto halves = [&] { return ++done == per ? (done = 0, last) : 2; };
-        Scales s0, s1;
-        if (stages) load(xs0, ys0, s0);
-        stage_arrived();
-        for (int s = 0; s < stages; s += 2) {
-            if (s + 1 < stages) load(xs1, ys1, s1);
-            multiply(xs0, ys0, halves(), s0);
-            stage_arrived();
-            if (s + 1 >= stages) break;
-            if (s + 2 < stages) load(xs0, ys0, s0);
-            multiply(xs1, ys1, halves(), s1);
-            stage_arrived();
+        if constexpr (PARTS) select();
+        // Loads of a stage in kSteps parts.  Behind the last stage they find nothing and bring zeros, so that every wavefront has as
+        // many loads under way as ever.
+        const int to = wave() * kWave * 16;
+        auto load = [&](char *ring, int step) {
+            lx.issue(rx.buffer(coming > 0), ring, to, step, kSteps);
+            ly.issue(ry.buffer(coming > 0), ring, kY + to, step, kSteps);
+            if (step + 1 < kSteps) return;
+            --coming;
+            rx.next();
+            ry.next();
+            if constexpr (PARTS)
+                if (--at == 0) {
+                    at = per;
+                    ++part;
+                    select();
+                }
+        };
+        i32x4 px[2][kQ], py[2][SY];             // of a step and of the next: x by the step, y by the stage
+        Scales scales{}, scales_next{};
+        uint32_t brought[2] = {};               // scales on their way to LDS, by the stage
+        const uint8_t *row = nullptr;
+        const int64_t groups = k1 / 32;
+        if constexpr (Mul::kScaled) {
+            const int t = threadIdx.x;
+            row = t < XT ? x.scales + lesser(i0 + t, x.rows - 1) * x.ld_scales : t < XT + YT ? y.scales + lesser(j0 + t - XT, y.rows - 1) * y.ld_scales : nullptr;
+            write_scales(scales0, load_scales(row, k0 / 32, groups));
+            write_scales(scales1, load_scales(row, k0 / 32 + 1, groups));
+            brought[0] = load_scales(row, k0 / 32 + 2, groups);
+            brought[1] = load_scales(row, k0 / 32 + 3, groups);
         }
+        auto load_all = [&](char *ring) {
+#pragma unroll
+            for (int step = 0; step < kSteps; ++step) load(ring, step);
+        };
+        load_all(ring0);
+        load_all(ring1);
+        load_all(ring2);
+        if (kSteps > 1) load(ring3, 0);
+        constexpr int kEach = LoadsX::kSurely + LoadsY::kSurely, kFirst = kSteps > 1 ? kEach / 2 : 0;
+        stage_arrived<2 * kEach + kFirst>();
+        read_step(ring0, 0, px[0], py[0]);
+        if constexpr (Mul::kScaled) read_scales(scales0, scales);
+        // Stage s out of `now`; `next` holds the next one, the second part of `later` is still to be asked for.
+        auto stage = [&](char *now, char *next, char *later, uint8_t *ss, uint8_t *sn, int parity, int s) {
+#pragma unroll
+            for (int step = 0; step < kSteps; ++step) {
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int kPerX = XS ? 2 : 1, kPerY = YS ? 2 : 1;
+                const int mine = kSteps == 1 ? parity : step & 1, coming = mine ^ 1;
+                if (step + 1 < kSteps) {
+                    read_step(now, step + 1, px[coming], py[parity]);
+                    load(later, step + 1);
+                } else {
+                    stage_arrived<(kSteps == 1 ? 1 : 2) * kEach>();      // the next stage's; what was asked for since then is on its way
+                    if constexpr (Mul::kScaled) {
+                        read_scales(sn, scales_next);                    // written before this barrier
+                        write_scales(ss, brought[parity]);               // stage s + 2's; what was there was read before it
+                        brought[parity] = load_scales(row, k0 / 32 + s + 4, groups);
+                    }
+                    read_step(next, 0, px[coming], py[parity ^ 1]);    // (after the last stage: zeros)
+                    load(kSteps == 1 ? later : now, 0);
+                }
+                multiply_step(px[mine], py[parity], step, scales);
+                if (step + 1 < kSteps) order_step<kQ * kPerX, kQ * SY>();
+                else order_step<kQ * kPerX + SY * kPerY, kQ * SY>();
+            }
+            if constexpr (Mul::kScaled) scales = scales_next;
+        };
+        for (int s = 0; s < stages; s += kRing) {
+            stage(ring0, ring1, ring3, scales0, scales1, 0, s);
+            if (s + 1 >= stages) break;
+            stage(ring1, ring2, ring0, scales1, scales0, 1, s + 1);
+            if (s + 2 >= stages) break;
+            stage(ring2, ring3, ring1, scales0, scales1, 0, s + 2);
+            if (s + 3 >= stages) break;
+            stage(ring3, ring0, ring2, scales1, scales0, 1, s + 3);
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);     // nothing is on its way to LDS any more
     }
 };
 

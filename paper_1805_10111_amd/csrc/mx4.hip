@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__re
             const float value = ldexpf(level, byte - 127);
             x[e >> 2][e & 3] = byte == 255 ? __uint_as_float(0x7fc00000u) : (code >> (4 * e)) & 8u ? -value : value;
         }
-        const int have = static_cast<int>(min<int64_t>(8, d - at * 8));
+        const int have = static_cast<int>(lesser(8, d - at * 8));
         typename Num<TYPE>::Mem *const to = out + r * ld + at * 8;
         store_four<TYPE>(to, x[0], min(have, 4), vector);
         if (have > 4) store_four<TYPE>(to + 4, x[1], have - 4, vector);
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void mx4_product_kernel(Operand w, O
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t i0 = static_cast<int64_t>(tx) * XT, j0 = static_cast<int64_t>(ty) * YT;
     Tile tile;
-    tile.run(w, a, i0, j0, 0, k, 1);
+    tile.template run<false>(w, a, i0, j0, 0, k);
 #pragma unroll
     for (int y = 0; y < Tile::SY; ++y) {
         const int64_t j = j0 + Tile::at_y(y);
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void mx4_product_kernel(Operand w, O
 #pragma unroll
         for (int m = 0; m < Tile::SX; ++m) {
             const int64_t i = i0 + Tile::at_x(m);
-            if (i < w.rows) store_four<TYPE>(out + j * ld + i, tile.acc[m][y], static_cast<int>(min<int64_t>(4, w.rows - i)), vector);
+            if (i < w.rows) store_four<TYPE>(out + j * ld + i, tile.acc[m][y], static_cast<int>(lesser(4, w.rows - i)), vector);
         }
     }
 }
