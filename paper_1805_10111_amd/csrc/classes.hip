@@ -2,7 +2,8 @@
 //
 // Both losses are sums  entropy_t + sum_j q_tj (lse_t - z_tj)  over a row's few targets (class, q): a label is one target of weight 1.
 // The scores z = a W^T / tau are made tile by tile and never stored:
-//   targets   the rows' targets in order of class, their weights q, which rows take part
+//   teacher   a teacher's entries in order of class, with their weights q
+//   pack      operands that the matrix cores cannot read in place
 //   scores    one tile of z: per row its maximum, the sum of exp above it and the targets' sum q z
 //   finish    lse and loss of a row from its tiles
 //   grad      (a piece of the classes at a time) the tile again, now g = f (exp(z - lse) - q), rounded to 16 bits
@@ -29,47 +30,92 @@ __device__ __forceinline__ void parts_of(float v, u16 out[3])
     out[2] = whole ? Part::store(r - Part::load(out[1])) : 0;
 }
 
-// ---- operands that are not read in place ---------------------------------------
-// Rows of [rows][cols] to rows of out_cols 16-bit numbers (three planes of them for float32), zeros behind row and column ends, and
-// in rows without a target where `cls` is given.  One thread per eight columns.
-template <int TYPE>
-__global__ __launch_bounds__(256) void pack_rows_kernel(const typename Num<TYPE>::Mem *__restrict__ v, int64_t ld, int64_t rows,
-                                                        int64_t cols, u16 *__restrict__ out, int64_t out_cols, int64_t out_rows,
-                                                        const int32_t *__restrict__ cls, int64_t k)
-{
-    const int64_t each = out_cols / 8, total = out_rows * each;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
-        const int64_t r = i / each, c = (i - r * each) * 8;
-        const bool live = r < rows && (!cls || cls[r * k] != kNoClass);
-        u16 part[3][8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const bool in = live && c + e < cols;
-            if constexpr (TYPE == DQ_F32) {
-                u16 p[3];
-                parts_of(in ? v[r * ld + c + e] : 0.0f, p);
-                part[0][e] = p[0];
-                part[1][e] = p[1];
-                part[2][e] = p[2];
-            } else {
-                part[0][e] = in ? v[r * ld + c + e] : 0;
-            }
+// ---- targets -------------------------------------------------------------------
+// What the kernels know of the rows' targets: k per row, sorted by class; q null for labels.  A class that is not one of the c is no
+// target (a label below 0, the end of a row's entries).
+struct Targets {
+    const int32_t *cls;
+    const float *q;
+    int32_t k;
+    uint32_t c;
+    // whether row t has a target: its first one is one
+    __device__ __forceinline__ bool used(int64_t t) const { return static_cast<uint32_t>(cls[t * k]) < c; }
+    // first target of row t with a class of at least c0
+    __device__ __forceinline__ int first(int64_t t, int c0) const
+    {
+        const int32_t *const row = cls + t * k;
+        int lo = 0, hi = k;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (row[mid] < c0) lo = mid + 1;
+            else hi = mid;
         }
+        return lo;
+    }
+};
+
+// ---- operands that are not read in place ---------------------------------------
+// Rows of [rows][cols] to rows of out_cols 16-bit numbers (three planes of them for float32), zeros behind row and column ends.
+// A second copy leaves out the rows without a target.  One thread per eight columns.
+struct Packed {
+    const void *v;
+    int64_t ld, rows, cols;
+    u16 *out, *used;                   // either may be null
+    int64_t out_rows, used_rows;       // with the zeros behind them
+    int vector;                        // rows that can be read 16 bytes at a time
+};
+template <int TYPE>
+__device__ __forceinline__ void pack_eight(const Packed &j, int64_t out_cols, int64_t i, const Targets &targets)
+{
+    typedef typename Num<TYPE>::Mem Mem;
+    const int64_t each = out_cols / 8, r = i / each, c = (i - r * each) * 8;
+    const Mem *const row = static_cast<const Mem *>(j.v) + r * j.ld;
+    u16 part[3][8];
+    Mem x[8] = {};
+    if (r < j.rows) {
+        if (j.vector && c + 8 <= j.cols) {
+            typedef __attribute__((ext_vector_type(16 / sizeof(Mem)))) Mem Wide;
 #pragma unroll
-        for (int p = 0; p < (TYPE == DQ_F32 ? 3 : 1); ++p)
-            *reinterpret_cast<i32x4 *>(out + p * out_rows * out_cols + r * out_cols + c) = __builtin_bit_cast(i32x4, part[p]);
+            for (int h = 0; h < static_cast<int>(sizeof(Mem)) / 2; ++h) {
+                const Wide w = *reinterpret_cast<const Wide *>(row + c + h * (16 / sizeof(Mem)));
+#pragma unroll
+                for (int e = 0; e < static_cast<int>(16 / sizeof(Mem)); ++e) x[h * (16 / sizeof(Mem)) + e] = w[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < j.cols) x[e] = row[c + e];
+        }
+    }
+    constexpr int kPlanes = TYPE == DQ_F32 ? 3 : 1;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (TYPE == DQ_F32) {
+            u16 p[3];
+            parts_of(x[e], p);
+            part[0][e] = p[0];
+            part[1][e] = p[1];
+            part[2][e] = p[2];
+        } else {
+            part[0][e] = x[e];
+        }
+    }
+    const bool live = j.used && r < j.rows && targets.used(r);
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p) {
+        const i32x4 v = __builtin_bit_cast(i32x4, part[p]);
+        if (j.out && r < j.out_rows) *reinterpret_cast<i32x4 *>(j.out + (p * j.out_rows + r) * out_cols + c) = v;
+        if (j.used && r < j.used_rows) *reinterpret_cast<i32x4 *>(j.used + (p * j.used_rows + r) * out_cols + c) = live ? v : i32x4{0, 0, 0, 0};
     }
 }
-
-// ---- targets -------------------------------------------------------------------
-__global__ __launch_bounds__(256) void label_kernel(const int32_t *__restrict__ label, int64_t n, int64_t c, int32_t *__restrict__ cls,
-                                                    uint32_t *__restrict__ status)
+// The features and the model in one launch.
+template <int TYPE>
+__global__ __launch_bounds__(256) void pack_kernel(Packed a, Packed w, int64_t out_cols, int64_t of_a, int64_t total, Targets targets)
 {
-    const int64_t t = blockIdx.x * 256ll + threadIdx.x;
-    if (t >= n) return;
-    const int32_t l = label[t];
-    if (l >= c && status) atomicOr(status, 2u);
-    cls[t] = l >= 0 && l < c ? l : kNoClass;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+        if (i < of_a) pack_eight<TYPE>(a, out_cols, i, targets);
+        else pack_eight<TYPE>(w, out_cols, i - of_a, targets);
+    }
 }
 
 // The largest |weight| of a call in float16, one block.
@@ -152,43 +198,22 @@ __global__ __launch_bounds__(kTeacherThreads) void teacher_kernel(const int32_t 
     }
 }
 
-// What the tile kernels know of the rows' targets: k per row, sorted by class, q null for labels.
-struct Targets {
-    const int32_t *cls;
-    const float *q;
-    int32_t k;
-};
-
-// first target of row t with a class of at least c0
-__device__ __forceinline__ int first_target(const Targets &g, int64_t t, int c0)
-{
-    const int32_t *cls = g.cls + t * g.k;
-    int lo = 0, hi = g.k;
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (cls[mid] < c0) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
-}
-
 // ---- scores --------------------------------------------------------------------
 __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
-// Sums of a tile's row are kept per wavefront column (slot): the row's maximum, the sum of exp above it, the targets' sum q z.
+// The sums of a tile's row: its maximum, the sum of exp above it, the targets' sum q z; [tile][row].
 template <int TYPE, int XT, int YT, int WX, int WY>
-__global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c,
-                                                               float inv_tau, Targets targets, int tiles_x, int tiles_y,
-                                                               float2 *__restrict__ sums, float *__restrict__ hits)
+__global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, float inv_tau, Targets targets,
+                                                               int tiles_x, int tiles_y, float2 *__restrict__ sums, float *__restrict__ hits)
 {
     typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false> Tile;
+    __shared__ float3 shared[WX][YT];
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t c0 = static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
     Tile tile;
     tile.template run<TYPE == DQ_F32>(w, a, c0, t0, 0, k);
     const int lane = threadIdx.x & 63, wave_c0 = static_cast<int>(c0) + Tile::sub_x(0) * 16;
-    const int64_t slot = static_cast<int64_t>(tx) * WX + Tile::wave() % WX;
 #pragma unroll
     for (int y = 0; y < Tile::SY; ++y) {
         const int64_t t = t0 + Tile::at_y(y);
@@ -217,7 +242,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operan
         if (live) {
             const int end = min(wave_c0 + Tile::SX * 16, static_cast<int>(c));
             const int32_t *cls = targets.cls + t * targets.k;
-            for (int e = first_target(targets, t, wave_c0); e < targets.k && cls[e] < end; ++e) {
+            for (int e = targets.first(t, wave_c0); e < targets.k && cls[e] < end; ++e) {
                 const int rel = cls[e] - base;
                 const float q = targets.q ? targets.q[t * targets.k + e] : 1.0f;
                 float z = 0.0f;
@@ -230,47 +255,72 @@ __global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operan
         }
         hit += __shfl_xor(hit, 16);
         hit += __shfl_xor(hit, 32);
-        if (live && lane < 16) {
-            sums[slot * n + t] = make_float2(top, sum);
-            hits[slot * n + t] = hit;
+        if (lane < 16) shared[Tile::wave() % WX][Tile::at_y(y)] = make_float3(top, sum, hit);
+    }
+    __syncthreads();
+    for (int r = threadIdx.x; r < YT && t0 + r < n; r += WX * WY * kWave) {
+        float top = -INFINITY, sum = 0.0f, hit = 0.0f;
+#pragma unroll
+        for (int x = 0; x < WX; ++x) top = fmaxf(top, shared[x][r].x);
+        const float from = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int x = 0; x < WX; ++x) {
+            const float3 v = shared[x][r];
+            sum += v.y * expf(v.x - from);
+            hit += v.z;
         }
+        sums[static_cast<int64_t>(tx) * n + t0 + r] = make_float2(top, sum);
+        hits[static_cast<int64_t>(tx) * n + t0 + r] = hit;
     }
 }
 
-// Sixteen rows a block, sixteen threads a row.
+// ROWS rows a block, 256 / ROWS threads a row.
+template <int ROWS>
 __global__ __launch_bounds__(256) void finish_kernel(const float2 *__restrict__ sums, const float *__restrict__ hits, int slots, int64_t n,
-                                                     const int32_t *__restrict__ cls, int32_t k, const float *__restrict__ entropy,
-                                                     float tau2, float *__restrict__ loss, float *__restrict__ lse_out,
-                                                     float *__restrict__ lse_kept, uint32_t *__restrict__ status)
+                                                     Targets targets, const float *__restrict__ entropy, float tau2, float *__restrict__ loss,
+                                                     float *__restrict__ lse_out, float *__restrict__ lse_kept, uint32_t *__restrict__ status)
 {
-    __shared__ float3 shared[16][16];
-    const int row = threadIdx.x & 15, part = threadIdx.x >> 4;
-    const int64_t t = blockIdx.x * 16ll + row;
-    float top = -INFINITY, sum = 0.0f, hit = 0.0f;
+    constexpr int kParts = 256 / ROWS;
+    __shared__ float tops[kParts][ROWS];
+    __shared__ float2 rest[kParts][ROWS];
+    const int row = threadIdx.x % ROWS, part = threadIdx.x / ROWS;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * ROWS + row;
+    float top = -INFINITY;
     if (t < n)
-        for (int s = part; s < slots; s += 16) {
+        for (int s = part; s < slots; s += kParts) top = fmaxf(top, sums[s * n + t].x);
+    tops[part][row] = top;
+    __syncthreads();
+    for (int o = kParts / 2; o; o /= 2) {
+        if (part < o) tops[part][row] = fmaxf(tops[part][row], tops[part + o][row]);
+        __syncthreads();
+    }
+    top = tops[0][row];
+    const float from = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, hit = 0.0f;
+    if (t < n)
+        for (int s = part; s < slots; s += kParts) {
             const float2 v = sums[s * n + t];
-            const float m = fmaxf(top, v.x), from = m == -INFINITY ? 0.0f : m;
-            sum = sum * expf(top - from) + v.y * expf(v.x - from);
-            top = m;
+            sum += v.y * expf(v.x - from);
             hit += hits[s * n + t];
         }
-    shared[part][row] = make_float3(top, sum, hit);
+    rest[part][row] = make_float2(sum, hit);
     __syncthreads();
-    if (part || t >= n) return;
-    for (int p = 1; p < 16; ++p) {
-        const float3 v = shared[p][row];
-        const float m = fmaxf(top, v.x), from = m == -INFINITY ? 0.0f : m;
-        sum = sum * expf(top - from) + v.y * expf(v.x - from);
-        top = m;
-        hit += v.z;
+    for (int o = kParts / 2; o; o /= 2) {
+        if (part < o) {
+            rest[part][row].x += rest[part + o][row].x;
+            rest[part][row].y += rest[part + o][row].y;
+        }
+        __syncthreads();
     }
-    const float lse = top + logf(sum);
-    const bool live = cls[t * k] != kNoClass;
-    if (loss) loss[t] = live ? tau2 * ((entropy ? entropy[t] : 0.0f) + (lse - hit)) : 0.0f;
+    if (part || t >= n) return;
+    const float lse = top + logf(rest[0][row].x);
+    const bool live = targets.used(t);
+    if (loss) loss[t] = live ? tau2 * ((entropy ? entropy[t] : 0.0f) + (lse - rest[0][row].y)) : 0.0f;
     if (lse_out) lse_out[t] = lse;
     if (lse_kept) lse_kept[t] = lse;
-    if (live && status && !__builtin_isfinite(lse)) atomicOr(status, 1u);
+    const bool far = !targets.q && targets.cls[t] >= static_cast<int64_t>(targets.c);       // (a teacher's were looked at before)
+    const uint32_t said = (live && !__builtin_isfinite(lse) ? 1u : 0u) | (far ? 2u : 0u);
+    if (said && status) atomicOr(status, said);
 }
 
 // ---- gradients -----------------------------------------------------------------
@@ -291,7 +341,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand 
 #pragma unroll
     for (int y = 0; y < Tile::SY; ++y) {
         const int64_t t = t0 + Tile::at_y(y);
-        const bool live = t < n && targets.cls[t * targets.k] != kNoClass;
+        const bool live = t < n && targets.used(t);
         const int base = static_cast<int>(c0) + Tile::at_x(0);
         const float from = live ? lse[t] : 0.0f;
         float f = live && weight ? weight[t] : 1.0f;
@@ -306,7 +356,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand 
         if (live) {
             const int end = min(wave_c0 + Tile::SX * 16, static_cast<int>(c));
             const int32_t *cls = targets.cls + t * targets.k;
-            for (int e = first_target(targets, t, wave_c0); e < targets.k && cls[e] < end; ++e) {
+            for (int e = targets.first(t, wave_c0); e < targets.k && cls[e] < end; ++e) {
                 const int rel = cls[e] - base;
                 const float q = targets.q ? targets.q[t * targets.k + e] : 1.0f;
 #pragma unroll
@@ -345,9 +395,12 @@ __device__ __forceinline__ float gradient_unit(int type, float post, const float
 }
 
 // da of a piece, one split of its classes per blockIdx.y: partial sums [split][n][ldp] in float32, added to what the pieces before left.
+// Where one launch has it all (partial null) da itself.
 template <int TYPE, int XT, int YT, int WX, int WY>
-__global__ __launch_bounds__(WX *WY *kWave) void da_kernel(Operand w, Operand g, int64_t piece, int64_t per_split, int64_t n, int tiles_x,
-                                                           int tiles_y, float *__restrict__ partial, int64_t ldp, int first)
+__global__ __launch_bounds__(WX *WY *kWave) void da_kernel(Operand w, Operand g, int64_t piece, int64_t per_split, int64_t n, int64_t d, int tiles_x,
+                                                           int tiles_y, float *__restrict__ partial, int64_t ldp, int first, Targets targets, float post,
+                                                           const float *__restrict__ weight_max, typename Num<TYPE>::Mem *__restrict__ da,
+                                                           int64_t ldda, int vector)
 {
     typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, false> Tile;
     int tx, ty;
@@ -358,24 +411,29 @@ __global__ __launch_bounds__(WX *WY *kWave) void da_kernel(Operand w, Operand g,
     Tile tile;
     tile.template run<TYPE == DQ_F32>(w, g, i0, t0, k0, k0 < k1 ? k1 : k0);
     float *const out = partial + blockIdx.y * n * ldp;
+    const float unit = gradient_unit(TYPE, post, weight_max);
 #pragma unroll
     for (int y = 0; y < Tile::SY; ++y) {
         const int64_t t = t0 + Tile::at_y(y);
         if (t >= n) continue;
+        const bool live = partial || targets.used(t);
 #pragma unroll
         for (int m = 0; m < Tile::SX; ++m) {
             const int64_t i = i0 + Tile::at_x(m);
-            if (i >= ldp) continue;
-            f32x4 *const to = reinterpret_cast<f32x4 *>(out + t * ldp + i);
-            *to = first ? tile.acc[m][y] : *to + tile.acc[m][y];
+            if (i >= d) continue;
+            if (partial) {
+                f32x4 *const to = reinterpret_cast<f32x4 *>(out + t * ldp + i);
+                *to = first ? tile.acc[m][y] : *to + tile.acc[m][y];
+            } else {
+                store_four<TYPE>(da + t * ldda + i, live ? tile.acc[m][y] * unit : f32x4{0.f, 0.f, 0.f, 0.f}, static_cast<int>(lesser(4, d - i)), vector);
+            }
         }
     }
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(256) void da_finish_kernel(const float *__restrict__ partial, int splits, int64_t n, int64_t d, int64_t ldp,
-                                                        const int32_t *__restrict__ cls, int32_t k, float post,
-                                                        const float *__restrict__ weight_max, typename Num<TYPE>::Mem *__restrict__ da,
+__global__ __launch_bounds__(256) void da_finish_kernel(const float *__restrict__ partial, int splits, int64_t n, int64_t d, int64_t ldp, Targets targets,
+                                                        float post, const float *__restrict__ weight_max, typename Num<TYPE>::Mem *__restrict__ da,
                                                         int64_t ldda, int vector)
 {
     const int64_t quads = (d + 3) / 4, total = n * quads;
@@ -383,7 +441,8 @@ __global__ __launch_bounds__(256) void da_finish_kernel(const float *__restrict_
     for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < total; at += gridDim.x * 256ll) {
         const int64_t t = at / quads, i = (at - t * quads) * 4;
         f32x4 v{0.f, 0.f, 0.f, 0.f};
-        if (cls[t * k] != kNoClass) {
+        if (targets.used(t)) {
+#pragma unroll 4
             for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x4 *>(partial + (s * n + t) * ldp + i);
             v *= unit;
         }
@@ -424,21 +483,36 @@ static inline int64_t room(int64_t &at, int64_t bytes)
     return here;
 }
 
+// Tiles of the products.  What a tile's side costs in the efficiency of the matrix cores it gains where there are few tiles: measured on
+// large products 256 x 256 reaches 1170 to 1330 TFLOP/s, 128 x 128 820 to 1120; 8192 rows of the smaller one's blocks, two to a compute
+// unit, take 1.4 times as long as the larger's for the same work.
+enum TileSize { kTile256, kTile128, kTile64, kTile16 };      // the last: 16 rows by 64 (classes) or 128 (columns)
+
+constexpr int side(TileSize s) { return s == kTile256 ? 256 : s == kTile128 ? 128 : s == kTile64 ? 64 : 16; }
+
+// The larger tile, unless the rounds its blocks take on 256 compute units are so much emptier than the smaller's that those are faster.
+static TileSize tile_for(int64_t x, int64_t y, int64_t copies)
+{
+    const int64_t big = (x + 255) / 256 * ((y + 255) / 256) * copies, small = (x + 127) / 128 * ((y + 127) / 128) * copies;
+    return 1.4 * 0.5 * static_cast<double>((small + 511) / 512) < static_cast<double>((big + 255) / 256) ? kTile128 : kTile256;
+}
+// ... of products over `rows` rows.
+static TileSize tile_for_rows(int64_t x, int64_t rows, int64_t copies)
+{
+    return rows <= 16 ? kTile16 : rows <= 64 ? kTile64 : tile_for(x, rows, copies);
+}
+
 // Sizes and places of everything a call passes through its workspace.
 struct ClassPlan {
     int32_t type, planes, wide;         // wide: bytes of a number in memory
     int64_t n, c, d, k, dp;             // dp: columns of packed rows
     bool direct_a, direct_w;
-    int yt;                             // rows of a tile
-    int64_t tiles_x, tiles_y, slots;
-    int64_t piece, pieces, ldg, rows_g, rows_z, splits, per_split;
+    TileSize tile, tile_da, tile_dw;
+    int64_t xt, yt, tiles_x, tiles_y;   // of scores
+    int64_t piece, pieces, ldg, rows_g, rows_z, xd, yd, splits, per_split;
+    bool da_at_once;
     int64_t cls, q, entropy, weight_max, lse, sums, hits, a, w, az, g, partial, bytes;
 };
-
-constexpr int kXT = 256;                 // classes of a tile
-
-// wavefronts along the classes of a tile of yt rows
-static int wave_cols(int yt) { return yt == 256 ? 2 : yt == 64 ? 4 : 8; }
 
 static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &s)
 {
@@ -458,52 +532,59 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
     s.d = p->d;
     s.k = k ? k : 1;
     s.dp = up(s.d, 64);
+    // The model is read in place where its rows are whole 16-byte chunks, also if they end inside of a step of 32 columns: what follows
+    // there meets the zeros behind the features' rows.  (Odd rows would lose the last number at the end of the memory.)
     s.direct_a = s.planes == 1 && s.d % 32 == 0 && p->lda % 8 == 0 && pa % 16 == 0;
-    s.direct_w = s.planes == 1 && s.d % 32 == 0 && p->ldw % 8 == 0 && pw % 16 == 0;
-    s.yt = s.n <= 16 ? 16 : s.n <= 64 ? 64 : 256;
-    s.tiles_x = (s.c + kXT - 1) / kXT;
+    s.direct_w = s.planes == 1 && s.d % 2 == 0 && p->ldw % 8 == 0 && pw % 16 == 0;
+    s.tile = tile_for_rows(s.c, s.n, 1);
+    s.yt = side(s.tile);
+    s.xt = s.tile == kTile16 ? 64 : s.yt;
+    s.tiles_x = (s.c + s.xt - 1) / s.xt;
     s.tiles_y = (s.n + s.yt - 1) / s.yt;
     if (s.tiles_x * s.tiles_y > kMost) return DQ_ERR_UNSUPPORTED;
-    s.slots = s.tiles_x * wave_cols(s.yt);
     int64_t at = 0;
-    s.cls = room(at, 4 * s.n * s.k);
+    s.cls = room(at, k ? 4 * s.n * s.k : 0);
     s.q = room(at, k ? 4 * s.n * s.k : 0);
     s.entropy = room(at, k ? 4 * s.n : 0);
     s.weight_max = room(at, 4);
     s.lse = room(at, 4 * s.n);
-    s.sums = room(at, 8 * s.slots * s.n);
-    s.hits = room(at, 4 * s.slots * s.n);
+    s.sums = room(at, 8 * s.tiles_x * s.n);
+    s.hits = room(at, 4 * s.tiles_x * s.n);
     s.a = room(at, s.direct_a ? 0 : 2 * s.planes * s.n * s.dp);
     s.w = room(at, s.direct_w ? 0 : 2 * s.planes * s.c * s.dp);
     if (grad) {
-        s.rows_z = up(s.n, 64);
+        s.rows_z = up(s.n, 32);
         s.rows_g = s.tiles_y * s.yt;
-        const int64_t most = std::max<int64_t>(kPieceBytes / (2 * s.planes * s.rows_g) / kXT, 1) * kXT;
+        const int64_t most = std::max<int64_t>(kPieceBytes / (2 * s.planes * s.rows_g) / 256, 1) * 256;
         s.pieces = (s.c + most - 1) / most;
-        s.piece = up((s.c + s.pieces - 1) / s.pieces, kXT);
+        s.piece = up((s.c + s.pieces - 1) / s.pieces, 256);
         s.pieces = (s.c + s.piece - 1) / s.piece;
         s.ldg = s.piece;
-        // da has few tiles: its classes are split until the chip is full, though not below eight stages each
-        const int64_t tiles = (s.d + kXT - 1) / kXT * s.tiles_y;
-        s.splits = std::clamp<int64_t>(512 / tiles, 1, std::max<int64_t>(s.piece / 512, 1));
-        s.per_split = up((s.piece + s.splits - 1) / s.splits, 64);
+        s.tile_dw = s.n <= 64 && s.c * s.d <= (1 << 20) ? kTile64 : tile_for(s.d, std::min(s.c, s.piece), 1);
+        // da has few tiles: its classes are split until the chip is full (a block per compute unit, smaller tiles two or more), though not
+        // below four steps each.
+        s.tile_da = s.n <= 16 ? kTile16 : s.n <= 64 ? kTile64 : s.n * s.d <= 256 * 1024 ? kTile128 : kTile256;
+        s.yd = side(s.tile_da);
+        s.xd = s.tile_da == kTile16 ? 128 : s.yd;
+        const int64_t tiles = (s.d + s.xd - 1) / s.xd * ((s.n + s.yd - 1) / s.yd), blocks = s.tile_da == kTile256 ? 256 : 512;
+        const int64_t most_splits = std::clamp<int64_t>(s.piece / 128, 1, std::max<int64_t>(blocks / tiles, 1));
+        s.splits = 1;
+        double best = 1e30;
+        for (int64_t i = 1; i <= most_splits; ++i) {         // fewest rounds for the work of one split, and something for its sums
+            const double cost = static_cast<double>((tiles * i + blocks - 1) / blocks) / static_cast<double>(i) * (1.0 + 0.01 * static_cast<double>(i));
+            if (cost < best) {
+                best = cost;
+                s.splits = i;
+            }
+        }
+        s.per_split = up((s.piece + s.splits - 1) / s.splits, 32);
         s.splits = (s.piece + s.per_split - 1) / s.per_split;
+        s.da_at_once = s.splits == 1 && s.pieces == 1;
         s.az = room(at, 2 * s.planes * s.rows_z * s.dp);
         s.g = room(at, 2 * s.planes * s.rows_g * s.ldg);
-        s.partial = room(at, 4 * s.splits * s.n * s.dp);
+        s.partial = room(at, s.da_at_once ? 0 : 4 * s.splits * s.n * s.dp);
     }
     s.bytes = up(at, 16);
-    return DQ_OK;
-}
-
-template <int TYPE>
-static int32_t pack_rows(const void *v, int64_t ld, int64_t rows, int64_t cols, char *out, int64_t out_cols, int64_t out_rows, const int32_t *cls,
-                         int64_t k, hipStream_t st)
-{
-    const int64_t blocks = std::min<int64_t>((out_rows * out_cols / 8 + 255) / 256, 1 << 16);
-    pack_rows_kernel<TYPE><<<static_cast<unsigned>(blocks), 256, 0, st>>>(static_cast<const typename Num<TYPE>::Mem *>(v), ld, rows, cols,
-                                                                          reinterpret_cast<u16 *>(out), out_cols, out_rows, cls, k);
-    DQ_LAUNCH_CHECK();
     return DQ_OK;
 }
 
@@ -524,49 +605,66 @@ struct ClassCall {
     hipStream_t st;
 };
 
-template <int TYPE, int YT, int WX, int WY>
+// One launch of a kernel template in the tile size that a plan names (wavefronts WX x WY); `few`: what it is launched as for 16 rows.
+#define DQ_TILE_LAUNCH(size, kernel, few, grid, ...)                                                               \
+    do {                                                                                                           \
+        switch (size) {                                                                                            \
+        case kTile256: kernel<TYPE, 256, 256, 2, 4><<<grid, 512, 0, st>>>(__VA_ARGS__); break;                     \
+        case kTile128: kernel<TYPE, 128, 128, 2, 2><<<grid, 256, 0, st>>>(__VA_ARGS__); break;                     \
+        case kTile64: kernel<TYPE, 64, 64, 2, 2><<<grid, 256, 0, st>>>(__VA_ARGS__); break;                        \
+        case kTile16: few<<<grid, 256, 0, st>>>(__VA_ARGS__); break;                                               \
+        }                                                                                                          \
+        DQ_LAUNCH_CHECK();                                                                                         \
+    } while (0)
+
+template <int TYPE>
 static int32_t class_run(const ClassCall &q, const ClassPlan &s)
 {
+    typedef typename Num<TYPE>::Mem Mem;
     const dq_classes &p = *q.prob;
     char *const ws = q.ws;
     const hipStream_t st = q.st;
     const int64_t n = s.n, c = s.c, wide = s.wide;
-    const unsigned threads = WX * WY * kWave;
-    int32_t *const cls = reinterpret_cast<int32_t *>(ws + s.cls);
     const float tau = q.teacher ? q.teacher->tau : 1.0f;
-    Targets targets{cls, nullptr, static_cast<int32_t>(s.k)};
+    Targets targets{q.label, nullptr, static_cast<int32_t>(s.k), static_cast<uint32_t>(c)};
     const float *entropy = nullptr;
     if (q.teacher) {
         int pow2 = 1;
         while (pow2 < s.k) pow2 *= 2;
+        int32_t *const cls = reinterpret_cast<int32_t *>(ws + s.cls);
         float *const tq = reinterpret_cast<float *>(ws + s.q), *const ent = reinterpret_cast<float *>(ws + s.entropy);
         teacher_kernel<<<static_cast<unsigned>(n), kTeacherThreads, 0, st>>>(q.teacher->cls, q.teacher->logit, q.teacher->ld, targets.k, pow2, c,
                                                                              1.0f / tau, cls, tq, ent, q.status);
+        DQ_LAUNCH_CHECK();
+        targets.cls = cls;
         targets.q = tq;
         entropy = ent;
-    } else {
-        label_kernel<<<static_cast<unsigned>((n + 255) / 256), 256, 0, st>>>(q.label, n, c, cls, q.status);
     }
-    DQ_LAUNCH_CHECK();
 
     // operands: in place, or packed
-    Operand a{static_cast<const char *>(p.a), p.lda * 2, n, 0, 0}, w{static_cast<const char *>(p.w), p.ldw * 2, c, static_cast<int32_t>(s.d), 0};
-    if (!s.direct_a) {
-        if (const int32_t e = pack_rows<TYPE>(p.a, p.lda, n, s.d, ws + s.a, s.dp, n, nullptr, 0, st)) return e;
-        a = Operand{ws + s.a, s.dp * 2, n, 0, n * s.dp * 2};
-    }
-    if (!s.direct_w) {
-        if (const int32_t e = pack_rows<TYPE>(p.w, p.ldw, c, s.d, ws + s.w, s.dp, c, nullptr, 0, st)) return e;
-        w = Operand{ws + s.w, s.dp * 2, c, static_cast<int32_t>(s.dp), c * s.dp * 2};
+    const bool want_dw = q.grad && q.dw;
+    const int32_t dp = static_cast<int32_t>(s.dp);
+    Operand a{static_cast<const char *>(p.a), p.lda * 2, n, static_cast<int32_t>(s.d), 0}, w{static_cast<const char *>(p.w), p.ldw * 2, c, static_cast<int32_t>(s.d), 0};
+    if (!s.direct_a) a = Operand{ws + s.a, s.dp * 2, n, dp, n * s.dp * 2};
+    if (!s.direct_w) w = Operand{ws + s.w, s.dp * 2, c, dp, c * s.dp * 2};
+    const Operand az{ws + s.az, s.dp * 2, s.rows_z, dp, s.rows_z * s.dp * 2};
+    const int64_t of_a = s.direct_a && !want_dw ? 0 : (want_dw ? s.rows_z : n) * s.dp / 8, of_w = s.direct_w ? 0 : c * s.dp / 8;
+    if (of_a + of_w) {
+        auto wide_rows = [&](const void *v, int64_t ld) { return aligned16(v) && ld * wide % 16 == 0; };
+        const Packed pa{p.a, p.lda, n, s.d, s.direct_a ? nullptr : reinterpret_cast<u16 *>(ws + s.a), want_dw ? reinterpret_cast<u16 *>(ws + s.az) : nullptr,
+                        n, s.rows_z, wide_rows(p.a, p.lda)};
+        const Packed pw{p.w, p.ldw, c, s.d, reinterpret_cast<u16 *>(ws + s.w), nullptr, c, 0, wide_rows(p.w, p.ldw)};
+        const int64_t blocks = std::min<int64_t>((of_a + of_w + 255) / 256, 1 << 16);
+        pack_kernel<TYPE><<<static_cast<unsigned>(blocks), 256, 0, st>>>(pa, pw, s.dp, of_a, of_a + of_w, targets);
+        DQ_LAUNCH_CHECK();
     }
     const int64_t kd = up(s.d, 32);
     float2 *const sums = reinterpret_cast<float2 *>(ws + s.sums);
     float *const hits = reinterpret_cast<float *>(ws + s.hits), *const lse = reinterpret_cast<float *>(ws + s.lse);
-    scores_kernel<TYPE, kXT, YT, WX, WY><<<static_cast<unsigned>(s.tiles_x * s.tiles_y), threads, 0, st>>>(
-        w, a, kd, n, c, 1.0f / tau, targets, static_cast<int>(s.tiles_x), static_cast<int>(s.tiles_y), sums, hits);
-    DQ_LAUNCH_CHECK();
-    finish_kernel<<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(sums, hits, static_cast<int>(s.slots), n, cls, targets.k, entropy, tau * tau,
-                                                                        q.loss, q.lse, q.grad ? lse : nullptr, q.status);
+    const int tiles_x = static_cast<int>(s.tiles_x), tiles_y = static_cast<int>(s.tiles_y);
+    DQ_TILE_LAUNCH(s.tile, scores_kernel, (scores_kernel<TYPE, 64, 16, 4, 1>), static_cast<unsigned>(tiles_x * tiles_y), w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits);
+    if (n <= 256) finish_kernel<1><<<static_cast<unsigned>(n), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
+    else finish_kernel<16><<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
     DQ_LAUNCH_CHECK();
     if (!q.grad || !(q.da || q.dw)) return DQ_OK;
 
@@ -577,53 +675,36 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
         weight_max_kernel<<<1, 1024, 0, st>>>(q.weight, n, weight_max);
         DQ_LAUNCH_CHECK();
     }
-    Operand az{ws + s.az, s.dp * 2, s.rows_z, static_cast<int32_t>(s.dp), s.rows_z * s.dp * 2};
-    if (q.dw)
-        if (const int32_t e = pack_rows<TYPE>(p.a, p.lda, n, s.d, ws + s.az, s.dp, s.rows_z, cls, s.k, st)) return e;
     u16 *const g = reinterpret_cast<u16 *>(ws + s.g);
-    float *const partial = reinterpret_cast<float *>(ws + s.partial);
+    float *const partial = s.da_at_once ? nullptr : reinterpret_cast<float *>(ws + s.partial);
     const int64_t plane = s.rows_g * s.ldg;
-    const int tiles_d = static_cast<int>((s.d + kXT - 1) / kXT);
-    typedef typename Num<TYPE>::Mem Mem;
+    const Operand go{reinterpret_cast<const char *>(g), s.ldg * 2, s.rows_g, static_cast<int32_t>(s.ldg), plane * 2};
+    const int vector_da = four_at_once(q.da, q.ldda, static_cast<int>(wide)), vector_dw = four_at_once(q.dw, q.lddw, static_cast<int>(wide));
+    Mem *const da = static_cast<Mem *>(q.da);
     for (int64_t at = 0; at < c; at += s.piece) {
         const int64_t have = std::min(s.piece, c - at);
-        const int tiles_p = static_cast<int>((have + kXT - 1) / kXT);
-        grad_kernel<TYPE, kXT, YT, WX, WY><<<static_cast<unsigned>(tiles_p * s.tiles_y), threads, 0, st>>>(
-            w, a, kd, n, c, at, have, 1.0f / tau, targets, lse, q.weight, weight_max, tiles_p, static_cast<int>(s.tiles_y), g, s.ldg, plane);
-        DQ_LAUNCH_CHECK();
-        const Operand along{reinterpret_cast<const char *>(g), s.ldg * 2, s.rows_g, 0, plane * 2};
+        const int tiles_p = static_cast<int>((have + s.xt - 1) / s.xt);
+        DQ_TILE_LAUNCH(s.tile, grad_kernel, (grad_kernel<TYPE, 64, 16, 4, 1>), static_cast<unsigned>(tiles_p * tiles_y), w, a, kd, n, c, at, have, 1.0f / tau, targets, lse, q.weight, weight_max,
+                       tiles_p, tiles_y, g, s.ldg, plane);
         if (q.da) {
             const Operand piece{w.p + at * w.ld, w.ld, c - at, w.cols, w.plane};
-            da_kernel<TYPE, kXT, YT, WX, WY><<<dim3(static_cast<unsigned>(tiles_d * s.tiles_y), static_cast<unsigned>(s.splits)), threads, 0, st>>>(
-                piece, along, up(have, 64), s.per_split, n, tiles_d, static_cast<int>(s.tiles_y), partial, s.dp, at == 0);
-            DQ_LAUNCH_CHECK();
+            const int tx = static_cast<int>((s.d + s.xd - 1) / s.xd), ty = static_cast<int>((n + s.yd - 1) / s.yd);
+            DQ_TILE_LAUNCH(s.tile_da, da_kernel, (da_kernel<TYPE, 128, 16, 4, 1>), dim3(static_cast<unsigned>(tx * ty), static_cast<unsigned>(s.splits)), piece, go, up(have, 32), s.per_split, n,
+                           s.d, tx, ty, partial, s.dp, at == 0, targets, post, weight_max, da, q.ldda, vector_da);
         }
         if (q.dw) {
-            const Operand across{reinterpret_cast<const char *>(g), s.ldg * 2, s.rows_g, static_cast<int32_t>(s.ldg), plane * 2};
-            dw_kernel<TYPE, kXT, 256, 2, 4><<<static_cast<unsigned>(tiles_d * tiles_p), 512, 0, st>>>(
-                az, across, up(n, 32), have, s.d, tiles_d, tiles_p, post, weight_max, static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw,
-                four_at_once(q.dw, q.lddw, static_cast<int>(wide)));
-            DQ_LAUNCH_CHECK();
+            const int t = side(s.tile_dw), tx = static_cast<int>((s.d + t - 1) / t), ty = static_cast<int>((have + t - 1) / t);
+            DQ_TILE_LAUNCH(s.tile_dw, dw_kernel, (dw_kernel<TYPE, 64, 64, 2, 2>), static_cast<unsigned>(tx * ty), az, go, s.rows_z, have, s.d, tx, ty, post, weight_max,
+                           static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw, vector_dw);
         }
     }
-    if (q.da) {
+    if (q.da && partial) {
         const int64_t blocks = std::min<int64_t>((n * ((s.d + 3) / 4) + 255) / 256, 1 << 16);
-        da_finish_kernel<TYPE><<<static_cast<unsigned>(blocks), 256, 0, st>>>(partial, static_cast<int>(s.splits), n, s.d, s.dp, cls, targets.k, post,
-                                                                              weight_max, static_cast<Mem *>(q.da), q.ldda,
-                                                                              four_at_once(q.da, q.ldda, static_cast<int>(wide)));
+        da_finish_kernel<TYPE><<<static_cast<unsigned>(blocks), 256, 0, st>>>(partial, static_cast<int>(s.splits), n, s.d, s.dp, targets, post, weight_max, da,
+                                                                              q.ldda, vector_da);
         DQ_LAUNCH_CHECK();
     }
     return DQ_OK;
-}
-
-template <int TYPE>
-static int32_t class_run_type(const ClassCall &q, const ClassPlan &s)
-{
-    switch (s.yt) {
-    case 16: return class_run<TYPE, 16, 8, 1>(q, s);
-    case 64: return class_run<TYPE, 64, 4, 2>(q, s);
-    default: return class_run<TYPE, 256, 2, 4>(q, s);
-    }
 }
 
 static int32_t class_call(ClassCall &q, void *ws, int64_t ws_bytes)
@@ -642,9 +723,9 @@ static int32_t class_call(ClassCall &q, void *ws, int64_t ws_bytes)
     if (ws_bytes < s.bytes) return DQ_ERR_WORKSPACE;
     q.ws = static_cast<char *>(ws);
     switch (s.type) {
-    case DQ_F32: return class_run_type<DQ_F32>(q, s);
-    case DQ_F16: return class_run_type<DQ_F16>(q, s);
-    default: return class_run_type<DQ_BF16>(q, s);
+    case DQ_F32: return class_run<DQ_F32>(q, s);
+    case DQ_F16: return class_run<DQ_F16>(q, s);
+    default: return class_run<DQ_BF16>(q, s);
     }
 }
 

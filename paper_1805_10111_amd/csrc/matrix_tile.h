@@ -39,7 +39,7 @@ struct Operand {
     const char *p;
     int64_t ld;            // bytes, a multiple of 16
     int64_t rows;
-    int32_t cols;          // stored across k: how many i there are; unused otherwise
+    int32_t cols;          // numbers of a row (pairs of bytes); even.  Along k: numbers of k behind them are zeros only in the last row
     int64_t plane;         // bytes from one part of a number to the next (float32 as three bfloat16), 0 otherwise
     const uint8_t *scales; // 4-bit numbers: four scales per 64 bytes of a row, from row to row ld_scales bytes
     int64_t ld_scales;
@@ -142,7 +142,7 @@ struct Reader {
     const char *p;
     int32_t left;                        // across k: rows from here on; along k: bytes from here to the end of the tile's last row
     int32_t ld, edge;                    // across k: bytes of a row, and by how much the last one is shorter
-    __device__ __forceinline__ Reader(const Operand &o, int64_t i0, int64_t k0, int64_t k1)
+    __device__ __forceinline__ Reader(const Operand &o, int64_t i0, int64_t k0)
     {
         ld = static_cast<int32_t>(o.ld);
         if constexpr (ACROSS) {
@@ -151,7 +151,7 @@ struct Reader {
             edge = static_cast<int32_t>(2 * (o.cols - i0) - o.ld);
         } else {
             p = o.p + i0 * o.ld + k0 * 2;
-            left = static_cast<int32_t>((lesser(o.rows - i0, T) - 1) * o.ld + 2 * (k1 - k0));
+            left = static_cast<int32_t>((lesser(o.rows - i0, T) - 1) * o.ld + 2 * (o.cols - k0));
             edge = 0;
         }
     }
@@ -304,8 +304,8 @@ struct TileProduct {
         if (stages <= 0) return;
         address_x = part_address<XT, XS>(sub_x(0));
         address_y = part_address<YT, YS>(sub_y(0));
-        const Reader<XT, XS> bx(x, i0, k0, k1);
-        const Reader<YT, YS> by(y, j0, k0, k1);
+        const Reader<XT, XS> bx(x, i0, k0);
+        const Reader<YT, YS> by(y, j0, k0);
         Reader<XT, XS> rx = bx;
         Reader<YT, YS> ry = by;
         int coming = stages, at = per, part = 0;     // stages to be loaded yet, of this product of parts

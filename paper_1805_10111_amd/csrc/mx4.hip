@@ -174,7 +174,7 @@ static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int64_t ld,
     constexpr int kXT = 256;
     const int64_t tiles_x = (w.n + kXT - 1) / kXT, tiles_y = (a.n + YT - 1) / YT;
     if (tiles_x * tiles_y > kMost4) return DQ_ERR_UNSUPPORTED;
-    auto operand = [](const dq_mx4 &q) { return Operand{reinterpret_cast<const char *>(q.codes), q.ld_codes, q.n, 0, 0, q.scales, q.ld_scales}; };
+    auto operand = [](const dq_mx4 &q) { return Operand{reinterpret_cast<const char *>(q.codes), q.ld_codes, q.n, static_cast<int32_t>(groups_of(q.d) * 32), 0, q.scales, q.ld_scales}; };
     mx4_product_kernel<TYPE, kXT, YT, WX, WY><<<static_cast<unsigned>(tiles_x * tiles_y), WX * WY * kWave, 0, st>>>(
         operand(w), operand(a), groups_of(a.d) * 32, static_cast<int>(tiles_x), static_cast<int>(tiles_y), static_cast<typename Num<TYPE>::Mem *>(out), ld,
         four_at_once(out, ld, wide_of(TYPE)));
