@@ -202,11 +202,11 @@ __global__ __launch_bounds__(kTeacherThreads) void teacher_kernel(const int32_t 
 __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // The sums of a tile's row: its maximum, the sum of exp above it, the targets' sum q z; [tile][row].
-template <int TYPE, int XT, int YT, int WX, int WY>
+template <int TYPE, int XT, int YT, int WX, int WY, int H>
 __global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, float inv_tau, Targets targets,
                                                                int tiles_x, int tiles_y, float2 *__restrict__ sums, float *__restrict__ hits)
 {
-    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false> Tile;
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H> Tile;
     __shared__ float3 shared[WX][YT];
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
@@ -325,13 +325,13 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2 *__restrict__ 
 
 // ---- gradients -----------------------------------------------------------------
 // g of a piece of the classes, [rows of the tiles][ldg] in 16 bits (three planes for float32); zeros where there is no row or class.
-template <int TYPE, int XT, int YT, int WX, int WY>
+template <int TYPE, int XT, int YT, int WX, int WY, int H>
 __global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, int64_t piece0,
                                                              int64_t piece, float inv_tau, Targets targets, const float *__restrict__ lse,
                                                              const float *__restrict__ weight, const float *__restrict__ weight_max,
                                                              int tiles_x, int tiles_y, u16 *__restrict__ g, int64_t ldg, int64_t plane)
 {
-    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false> Tile;
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H> Tile;
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t c0 = piece0 + static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
@@ -396,13 +396,13 @@ __device__ __forceinline__ float gradient_unit(int type, float post, const float
 
 // da of a piece, one split of its classes per blockIdx.y: partial sums [split][n][ldp] in float32, added to what the pieces before left.
 // Where one launch has it all (partial null) da itself.
-template <int TYPE, int XT, int YT, int WX, int WY>
+template <int TYPE, int XT, int YT, int WX, int WY, int H>
 __global__ __launch_bounds__(WX *WY *kWave) void da_kernel(Operand w, Operand g, int64_t piece, int64_t per_split, int64_t n, int64_t d, int tiles_x,
                                                            int tiles_y, float *__restrict__ partial, int64_t ldp, int first, Targets targets, float post,
                                                            const float *__restrict__ weight_max, typename Num<TYPE>::Mem *__restrict__ da,
                                                            int64_t ldda, int vector)
 {
-    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, false> Tile;
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, false, H> Tile;
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t i0 = static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT, k0 = blockIdx.y * per_split;
@@ -450,12 +450,12 @@ __global__ __launch_bounds__(256) void da_finish_kernel(const float *__restrict_
     }
 }
 
-template <int TYPE, int XT, int YT, int WX, int WY>
+template <int TYPE, int XT, int YT, int WX, int WY, int H>
 __global__ __launch_bounds__(WX *WY *kWave) void dw_kernel(Operand a, Operand g, int64_t k, int64_t piece, int64_t d, int tiles_x, int tiles_y,
                                                            float post, const float *__restrict__ weight_max,
                                                            typename Num<TYPE>::Mem *__restrict__ dw, int64_t lddw, int vector)
 {
-    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, true> Tile;
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, true, H> Tile;
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t i0 = static_cast<int64_t>(tx) * XT, j0 = static_cast<int64_t>(ty) * YT;
@@ -481,25 +481,6 @@ static inline int64_t room(int64_t &at, int64_t bytes)
     const int64_t here = at;
     at = up(at + bytes, 256);
     return here;
-}
-
-// Tiles of the products.  What a tile's side costs in the efficiency of the matrix cores it gains where there are few tiles: measured on
-// large products 256 x 256 reaches 1170 to 1330 TFLOP/s, 128 x 128 820 to 1120; 8192 rows of the smaller one's blocks, two to a compute
-// unit, take 1.4 times as long as the larger's for the same work.
-enum TileSize { kTile256, kTile128, kTile64, kTile16 };      // the last: 16 rows by 64 (classes) or 128 (columns)
-
-constexpr int side(TileSize s) { return s == kTile256 ? 256 : s == kTile128 ? 128 : s == kTile64 ? 64 : 16; }
-
-// The larger tile, unless the rounds its blocks take on 256 compute units are so much emptier than the smaller's that those are faster.
-static TileSize tile_for(int64_t x, int64_t y, int64_t copies)
-{
-    const int64_t big = (x + 255) / 256 * ((y + 255) / 256) * copies, small = (x + 127) / 128 * ((y + 127) / 128) * copies;
-    return 1.4 * 0.5 * static_cast<double>((small + 511) / 512) < static_cast<double>((big + 255) / 256) ? kTile128 : kTile256;
-}
-// ... of products over `rows` rows.
-static TileSize tile_for_rows(int64_t x, int64_t rows, int64_t copies)
-{
-    return rows <= 16 ? kTile16 : rows <= 64 ? kTile64 : tile_for(x, rows, copies);
 }
 
 // Sizes and places of everything a call passes through its workspace.
@@ -536,7 +517,7 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
     // there meets the zeros behind the features' rows.  (Odd rows would lose the last number at the end of the memory.)
     s.direct_a = s.planes == 1 && s.d % 32 == 0 && p->lda % 8 == 0 && pa % 16 == 0;
     s.direct_w = s.planes == 1 && s.d % 2 == 0 && p->ldw % 8 == 0 && pw % 16 == 0;
-    s.tile = tile_for_rows(s.c, s.n, 1);
+    s.tile = tile_for_rows(s.c, s.n);
     s.yt = side(s.tile);
     s.xt = s.tile == kTile16 ? 64 : s.yt;
     s.tiles_x = (s.c + s.xt - 1) / s.xt;
@@ -560,7 +541,7 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
         s.piece = up((s.c + s.pieces - 1) / s.pieces, 256);
         s.pieces = (s.c + s.piece - 1) / s.piece;
         s.ldg = s.piece;
-        s.tile_dw = s.n <= 64 && s.c * s.d <= (1 << 20) ? kTile64 : tile_for(s.d, std::min(s.c, s.piece), 1);
+        s.tile_dw = s.n <= 64 && s.c * s.d <= (1 << 20) ? kTile64 : tile_for(s.d, std::min(s.c, s.piece));
         // da has few tiles: its classes are split until the chip is full (a block per compute unit, smaller tiles two or more), though not
         // below four steps each.
         s.tile_da = s.n <= 16 ? kTile16 : s.n <= 64 ? kTile64 : s.n * s.d <= 256 * 1024 ? kTile128 : kTile256;
@@ -605,13 +586,14 @@ struct ClassCall {
     hipStream_t st;
 };
 
-// One launch of a kernel template in the tile size that a plan names (wavefronts WX x WY); `few`: what it is launched as for 16 rows.
+// One launch of a kernel template in the tile size that a plan names (wavefronts WX x WY, steps a stage); `few`: what it is launched as
+// for 16 rows.
 #define DQ_TILE_LAUNCH(size, kernel, few, grid, ...)                                                               \
     do {                                                                                                           \
         switch (size) {                                                                                            \
-        case kTile256: kernel<TYPE, 256, 256, 2, 4><<<grid, 512, 0, st>>>(__VA_ARGS__); break;                     \
-        case kTile128: kernel<TYPE, 128, 128, 2, 2><<<grid, 256, 0, st>>>(__VA_ARGS__); break;                     \
-        case kTile64: kernel<TYPE, 64, 64, 2, 2><<<grid, 256, 0, st>>>(__VA_ARGS__); break;                        \
+        case kTile256: kernel<TYPE, 256, 256, 2, 4, 1><<<grid, 512, 0, st>>>(__VA_ARGS__); break;                     \
+        case kTile128: kernel<TYPE, 128, 128, 2, 2, 1><<<grid, 256, 0, st>>>(__VA_ARGS__); break;                     \
+        case kTile64: kernel<TYPE, 64, 64, 2, 2, 2><<<grid, 256, 0, st>>>(__VA_ARGS__); break;                        \
         case kTile16: few<<<grid, 256, 0, st>>>(__VA_ARGS__); break;                                               \
         }                                                                                                          \
         DQ_LAUNCH_CHECK();                                                                                         \
@@ -662,7 +644,7 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     float2 *const sums = reinterpret_cast<float2 *>(ws + s.sums);
     float *const hits = reinterpret_cast<float *>(ws + s.hits), *const lse = reinterpret_cast<float *>(ws + s.lse);
     const int tiles_x = static_cast<int>(s.tiles_x), tiles_y = static_cast<int>(s.tiles_y);
-    DQ_TILE_LAUNCH(s.tile, scores_kernel, (scores_kernel<TYPE, 64, 16, 4, 1>), static_cast<unsigned>(tiles_x * tiles_y), w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits);
+    DQ_TILE_LAUNCH(s.tile, scores_kernel, (scores_kernel<TYPE, 64, 16, 4, 1, 2>), static_cast<unsigned>(tiles_x * tiles_y), w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits);
     if (n <= 256) finish_kernel<1><<<static_cast<unsigned>(n), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
     else finish_kernel<16><<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
     DQ_LAUNCH_CHECK();
@@ -684,17 +666,17 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     for (int64_t at = 0; at < c; at += s.piece) {
         const int64_t have = std::min(s.piece, c - at);
         const int tiles_p = static_cast<int>((have + s.xt - 1) / s.xt);
-        DQ_TILE_LAUNCH(s.tile, grad_kernel, (grad_kernel<TYPE, 64, 16, 4, 1>), static_cast<unsigned>(tiles_p * tiles_y), w, a, kd, n, c, at, have, 1.0f / tau, targets, lse, q.weight, weight_max,
+        DQ_TILE_LAUNCH(s.tile, grad_kernel, (grad_kernel<TYPE, 64, 16, 4, 1, 2>), static_cast<unsigned>(tiles_p * tiles_y), w, a, kd, n, c, at, have, 1.0f / tau, targets, lse, q.weight, weight_max,
                        tiles_p, tiles_y, g, s.ldg, plane);
         if (q.da) {
             const Operand piece{w.p + at * w.ld, w.ld, c - at, w.cols, w.plane};
             const int tx = static_cast<int>((s.d + s.xd - 1) / s.xd), ty = static_cast<int>((n + s.yd - 1) / s.yd);
-            DQ_TILE_LAUNCH(s.tile_da, da_kernel, (da_kernel<TYPE, 128, 16, 4, 1>), dim3(static_cast<unsigned>(tx * ty), static_cast<unsigned>(s.splits)), piece, go, up(have, 32), s.per_split, n,
+            DQ_TILE_LAUNCH(s.tile_da, da_kernel, (da_kernel<TYPE, 128, 16, 4, 1, 2>), dim3(static_cast<unsigned>(tx * ty), static_cast<unsigned>(s.splits)), piece, go, up(have, 32), s.per_split, n,
                            s.d, tx, ty, partial, s.dp, at == 0, targets, post, weight_max, da, q.ldda, vector_da);
         }
         if (q.dw) {
             const int t = side(s.tile_dw), tx = static_cast<int>((s.d + t - 1) / t), ty = static_cast<int>((have + t - 1) / t);
-            DQ_TILE_LAUNCH(s.tile_dw, dw_kernel, (dw_kernel<TYPE, 64, 64, 2, 2>), static_cast<unsigned>(tx * ty), az, go, s.rows_z, have, s.d, tx, ty, post, weight_max,
+            DQ_TILE_LAUNCH(s.tile_dw, dw_kernel, (dw_kernel<TYPE, 64, 64, 2, 2, 2>), static_cast<unsigned>(tx * ty), az, go, s.rows_z, have, s.d, tx, ty, post, weight_max,
                            static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw, vector_dw);
         }
     }

@@ -7,8 +7,9 @@
 //
 // Either operand is stored along k (row-major rows i, k contiguous), or across it (row-major rows k, i contiguous); the latter
 // reaches the matrix cores through the transposing reads of LDS, so nothing is ever transposed in memory.
-// A stage is 64 bytes of k: 32 numbers of 16 bits, 128 of 4.  LDS holds a ring of four, filled by loads that go there directly: while
-// one is multiplied, three are on their way.
+// A step is 64 bytes of k: 32 numbers of 16 bits, 128 of 4; a stage is H steps.  LDS holds a ring of four stages, filled by loads that
+// go there directly: while one is multiplied, three are on their way.  One step is right where the matrix cores bound (large tiles,
+// short stages); where memory does (few rows), rows are read 128 bytes at a time and more.
 //
 // What bounds it: the matrix cores.  256 x 256 with eight wavefronts (a wavefront multiplies 128 x 64: 12 reads of LDS for 32
 // products) needs 96 KB of LDS reads per 1024 cycles of matrix-core work, and each byte of memory is used for 256 products.
@@ -29,9 +30,9 @@ typedef __attribute__((ext_vector_type(8))) short i16x8;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 
-constexpr int kStageBytes = 64;                // of k, per row of an operand stored along k
-constexpr int kStageRows = 32;                 // of k, for an operand stored across it (16-bit numbers)
-constexpr int kRing = 4;                       // stages in LDS
+constexpr int kStepBytes = 64;                 // of k in a product of the matrix cores, per row of an operand stored along k
+constexpr int kStepRows = 32;                  // of k, for an operand stored across it (16-bit numbers)
+constexpr int kRing = 4;                       // stages in LDS, of H steps each
 
 // An operand in memory.  Its row i (row k where it is stored across k) begins at p + i * ld bytes; rows is how many there are.
 // Nothing outside of it is read: rows past the last are zeros, and k past its end.
@@ -101,15 +102,24 @@ __device__ __forceinline__ void stage_arrived()
 
 // The loads of one operand's stages.  ACROSS: stored across k.
 // LDS holds a stage as it lies in memory, its 16-byte chunks permuted within a row so that no two of the lanes that read together
-// meet a bank: along k, chunk c of row r at c ^ (r / 4) % 4 (16 lanes read 16 rows of 64 bytes); across k, 32 bytes at a time,
+// meet a bank: along k, chunk c of row r at c ^ (r H / 4) % 4H (16 lanes read 16 rows of 64 H bytes); across k, 32 bytes at a time,
 // pair c of row k at c ^ (k % 4 + 4 (k / 8 % 2)) (32 lanes read rows k .. k + 3 and k + 8 .. k + 11).
-template <int T, bool ACROSS, int THREADS>
+template <int T, bool ACROSS, int THREADS, int H>
 struct StageLoads {
-    static constexpr int kChunks = (T * 4 + THREADS - 1) / THREADS;              // loads of a thread per stage
-    static constexpr int kSurely = T * 4 / THREADS;                              // ... of any thread
-    static constexpr int kRowChunks = ACROSS ? T / 8 : 4;
+    static constexpr int kAll = T * 4 * H;                                       // 16-byte chunks of a stage
+    static constexpr int kChunks = (kAll + THREADS - 1) / THREADS;               // loads of a thread per stage
+    static constexpr int kSurely = kAll / THREADS;                               // ... of any thread
+    static constexpr int kRowChunks = ACROSS ? T / 8 : 4 * H;
     static constexpr int kPairMask = T / 16 >= 8 ? 7 : T / 16 - 1;
     uint32_t off[kChunks];
+
+    // loads of any thread in the first of `slices` slices
+    static constexpr int first(int slices)
+    {
+        int n = 0;
+        for (int i = 0; i < kSurely; ++i) n += i * slices / kChunks == 0;
+        return n;
+    }
 
     __device__ __forceinline__ void init(const Operand &o)
     {
@@ -118,18 +128,24 @@ struct StageLoads {
             const int id = threadIdx.x + i * THREADS, row = id / kRowChunks, slot = id % kRowChunks;
             int at;
             if constexpr (ACROSS) at = (((slot >> 1) ^ (((row & 3) | ((row >> 1) & 4)) & kPairMask)) * 2 + (slot & 1)) * 16;
-            else at = (slot ^ ((row >> 2) & 3)) * 16;
+            else at = (slot ^ ((row * H / 4) & (4 * H - 1))) * 16;
             off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(o.ld) + static_cast<uint32_t>(at);
         }
     }
-    // `part` of `parts` of the loads; to: where this wavefront's first one goes.
-    __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t from, char *ring, int to, int part, int parts) const
+    // `part` of `parts` of the loads; to: where this wavefront's first one goes.  wide: bytes of k there are yet; a stage of several
+    // steps may end behind them, and what lies there, in the next row, is not read but zeros are.
+    __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t from, char *ring, int to, int part, int parts, int wide) const
     {
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
             if (i * parts / kChunks != part) continue;
-            if (kChunks != kSurely && static_cast<int>(threadIdx.x) + i * THREADS >= T * 4) continue;      // (whole wavefronts)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (LdsPtr)(ring + (to + i * THREADS * 16)), 16, static_cast<int>(off[i]), 0, 0, 0);
+            if (kChunks != kSurely && static_cast<int>(threadIdx.x) + i * THREADS >= kAll) continue;      // (whole wavefronts)
+            uint32_t at = off[i];
+            if constexpr (H > 1 && !ACROSS) {
+                const int id = threadIdx.x + i * THREADS, row = id / kRowChunks;
+                if (((id % kRowChunks) ^ ((row * H / 4) & (4 * H - 1))) * 16 >= wide) at = 0x7fffffff;      // behind every buffer
+            }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (LdsPtr)(ring + (to + i * THREADS * 16)), 16, static_cast<int>(at), 0, 0, 0);
         }
     }
 };
@@ -137,7 +153,7 @@ struct StageLoads {
 // Where an operand's next stage lies: a buffer, behind whose end everything reads as zero.  (Loads to LDS go through buffers also
 // because the compiler takes those through plain pointers for possible accesses to LDS by address, and then waits for all reads of
 // LDS at every use of one.)  Moving on takes a few scalar instructions.
-template <int T, bool ACROSS>
+template <int T, bool ACROSS, int H>
 struct Reader {
     const char *p;
     int32_t left;                        // across k: rows from here on; along k: bytes from here to the end of the tile's last row
@@ -158,18 +174,18 @@ struct Reader {
     // any: whether there is another stage
     __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(bool any) const
     {
-        const int32_t bytes = ACROSS ? max(min(left, kStageRows) * ld + edge, 0) : left;
+        const int32_t bytes = max(ACROSS ? min(left, kStepRows * H) * ld + edge : left, 0);
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p), 0, any ? bytes : 0, 0x00027000);
     }
     __device__ __forceinline__ void next()
     {
-        p += ACROSS ? static_cast<int64_t>(kStageRows) * ld : kStageBytes;
-        left -= ACROSS ? kStageRows : kStageBytes;
+        p += ACROSS ? static_cast<int64_t>(kStepRows * H) * ld : kStepBytes * H;
+        left -= ACROSS ? kStepRows * H : kStepBytes * H;
     }
 };
 
 // Where in an operand's part of a stage a lane reads of subtile 0 of those of its wavefront (subtiles first ..).
-template <int T, bool ACROSS>
+template <int T, bool ACROSS, int H>
 __device__ __forceinline__ int part_address(int first)
 {
     const int lane = threadIdx.x & (kWave - 1), j = lane & 15, g = lane >> 4;
@@ -177,26 +193,27 @@ __device__ __forceinline__ int part_address(int first)
         constexpr int mask = T / 16 >= 8 ? 7 : T / 16 - 1;
         return (g * 8 + (j >> 2)) * (T * 2) + ((first ^ (((j >> 2) | ((g & 1) << 2)) & mask)) * 32) + (j & 3) * 8;
     } else {
-        return (first * 16 + j) * kStageBytes + ((g ^ (j >> 2)) * 16);
+        return (first * 16 + j) * kStepBytes * H + ((g ^ ((j * H / 4) & (4 * H - 1))) * 16);
     }
 }
-// ... and what it reads of subtile m of them (there are a power of two of them, their first a multiple of it).  An operand's part of the
+// ... and what it reads of step `half` and subtile m of them (there are a power of two of them, their first a multiple of it).  An operand's part of the
 // ring begins `from` in.  (One addition to the array: the compiler follows an address to its array through a few additions only.)
-template <int T, bool ACROSS>
-__device__ __forceinline__ i32x4 stage_part(const char *ring, int from, int address, int m)
+template <int T, bool ACROSS, int H>
+__device__ __forceinline__ i32x4 stage_part(const char *ring, int from, int address, int half, int m)
 {
     if constexpr (ACROSS) {
         const int at = address ^ (m * 32);
+        from += half * kStepRows * T * 2;
         const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(ring + (from + at)));
         const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(ring + (from + 4 * T * 2 + at)));
         return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-        return *reinterpret_cast<const i32x4 *>(ring + (from + m * 16 * kStageBytes + address));
+        return *reinterpret_cast<const i32x4 *>(ring + (from + m * 16 * kStepBytes * H + (address ^ (half * kStepBytes))));
     }
 }
 
 // WX x WY wavefronts share the tile.  Each of them multiplies SX x SY subtiles.
-template <class Mul, int XT, int YT, int WX, int WY, bool XS, bool YS>
+template <class Mul, int XT, int YT, int WX, int WY, bool XS, bool YS, int H = 1>
 struct TileProduct {
     static constexpr int kThreads = WX * WY * kWave;
     static constexpr int SX = XT / 16 / WX, SY = YT / 16 / WY;
@@ -210,12 +227,15 @@ struct TileProduct {
     static __device__ __forceinline__ int at_x(int m) { return sub_x(m) * 16 + ((threadIdx.x & 63) >> 4) * 4; }
     static __device__ __forceinline__ int at_y(int n) { return sub_y(n) * 16 + (threadIdx.x & 15); }
 
-    // Scales of 4-bit numbers.  A stage has four blocks a row; LDS holds their scales as [block][row % 16][row / 16], so that what a
+    // Scales of 4-bit numbers.  A step has four blocks a row; LDS holds their scales as [block][row % 16][row / 16], so that what a
     // lane needs for its subtiles are neighbouring bytes.  Thread r brings those of row r (x's rows, then y's).
-    static constexpr int kScaleBytes = 4 * (XT + YT);
+    static constexpr int kScaleBytes = 4 * (XT + YT);       // of a step
     static_assert(!Mul::kScaled || XT + YT <= kThreads, "a thread brings one row's scales");
     struct Scales {
-        uint32_t x[(SX + 3) / 4], y[(SY + 3) / 4];
+        uint32_t x[H][(SX + 3) / 4], y[H][(SY + 3) / 4];
+    };
+    struct Brought {
+        uint32_t v[H];
     };
     template <int S, int T>
     static __device__ __forceinline__ void read_scales(const uint8_t *lds, int sub, uint32_t (&out)[(S + 3) / 4])
@@ -228,50 +248,60 @@ struct TileProduct {
     }
     static __device__ __forceinline__ void read_scales(const uint8_t *lds, Scales &s)
     {
-        read_scales<SX, XT>(lds, sub_x(0), s.x);
-        read_scales<SY, YT>(lds + 4 * XT, sub_y(0), s.y);
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            read_scales<SX, XT>(lds + h * kScaleBytes, sub_x(0), s.x[h]);
+            read_scales<SY, YT>(lds + h * kScaleBytes + 4 * XT, sub_y(0), s.y[h]);
+        }
     }
-    static __device__ __forceinline__ uint32_t load_scales(const uint8_t *row, int64_t group, int64_t groups)
+    static __device__ __forceinline__ Brought load_scales(const uint8_t *row, int64_t stage, int64_t groups)
     {
-        return row ? *reinterpret_cast<const uint32_t *>(row + lesser(group, groups - 1) * 4) : 0;
+        Brought b;
+#pragma unroll
+        for (int h = 0; h < H; ++h) b.v[h] = row ? *reinterpret_cast<const uint32_t *>(row + lesser(stage * H + h, groups - 1) * 4) : 0;
+        return b;
     }
-    static __device__ __forceinline__ void write_scales(uint8_t *lds, uint32_t v)
+    static __device__ __forceinline__ void write_scales(uint8_t *lds, const Brought &b)
     {
         const bool in_x = threadIdx.x < XT;
         const int r = in_x ? threadIdx.x : threadIdx.x - XT, rows = in_x ? XT : YT;
         if (r >= rows) return;
         uint8_t *const at = lds + (in_x ? 0 : 4 * XT) + (r & 15) * (rows / 16) + (r >> 4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) at[i * rows] = static_cast<uint8_t>(v >> (8 * i));
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) at[h * kScaleBytes + i * rows] = static_cast<uint8_t>(b.v[h] >> (8 * i));
     }
 
-    // A stage is multiplied in steps of kQ of x's subtiles; what a step multiplies has been read from LDS a step before.
-    static constexpr int kQ = SX < 4 ? SX : 4, kSteps = SX / kQ;
-    static constexpr int kY = XT * kStageBytes;     // where y's part of a stage begins
-    __device__ __forceinline__ void read_step(const char *ring, int step, i32x4 (&x)[kQ], i32x4 (&y)[SY]) const
+    // A stage is multiplied in parts: H steps, kQ of x's subtiles at a time; what a part multiplies has been read from LDS a part before.
+    static constexpr int kQ = SX < 4 ? SX : 4, kPer = SX / kQ, kParts = H * kPer;
+    static constexpr int kY = XT * kStepBytes * H;           // where y's part of a stage begins
+    __device__ __forceinline__ void read_part(const char *ring, int part, i32x4 (&x)[kQ], i32x4 (&y)[SY]) const
     {
-        if (step == 0)
+        const int half = part / kPer, q = part % kPer;
+        if (q == 0)
 #pragma unroll
-            for (int n = 0; n < SY; ++n) y[n] = stage_part<YT, YS>(ring, kY, address_y, n);
+            for (int n = 0; n < SY; ++n) y[n] = stage_part<YT, YS, H>(ring, kY, address_y, half, n);
 #pragma unroll
-        for (int m = 0; m < kQ; ++m) x[m] = stage_part<XT, XS>(ring, 0, address_x, step * kQ + m);
+        for (int m = 0; m < kQ; ++m) x[m] = stage_part<XT, XS, H>(ring, 0, address_x, half, q * kQ + m);
     }
-    __device__ __forceinline__ void multiply_step(const i32x4 (&x)[kQ], const i32x4 (&y)[SY], int step, const Scales &scales)
+    __device__ __forceinline__ void multiply_part(const i32x4 (&x)[kQ], const i32x4 (&y)[SY], int part, const Scales &scales)
     {
+        const int half = part / kPer, q = part % kPer;
 #pragma unroll
         for (int m = 0; m < kQ; ++m)
 #pragma unroll
             for (int n = 0; n < SY; ++n) {
-                f32x4 &c = acc[step * kQ + m][n];
-                const int at = step * kQ + m;
-                if constexpr (Mul::kScaled) c = Mul::mul(x[m], y[n], c, static_cast<int>(scales.x[at / 4]), at % 4, static_cast<int>(scales.y[n / 4]), n % 4);
+                const int at = q * kQ + m;
+                f32x4 &c = acc[at][n];
+                if constexpr (Mul::kScaled) c = Mul::mul(x[m], y[n], c, static_cast<int>(scales.x[half][at / 4]), at % 4, static_cast<int>(scales.y[half][n / 4]), n % 4);
                 else c = Mul::mul(x[m], y[n], c);
             }
     }
-    // In what order a step's instructions are issued: the next step's reads of LDS between the first products, so that each has the
-    // rest of the step to arrive (left to itself the compiler puts them right before their use).
+    // In what order a part's instructions are issued: the next part's reads of LDS between the first products, so that each has the
+    // rest of the part to arrive (left to itself the compiler puts them right before their use).
     template <int READS, int PRODUCTS>
-    static __device__ __forceinline__ void order_step()
+    static __device__ __forceinline__ void order_part()
     {
         constexpr int kLds = 0x100, kMatrix = 0x8, kEach = READS > PRODUCTS ? 1 : PRODUCTS / READS > 2 ? 2 : 1;
 #pragma unroll
@@ -287,11 +317,11 @@ struct TileProduct {
     __device__ __forceinline__ void run(const Operand &x, const Operand &y, int64_t i0, int64_t j0, int64_t k0, int64_t k1)
     {
         // (an array of its own for each stage: the compiler keeps apart what is read and what is arriving by the array, up to seven)
-        __shared__ __attribute__((aligned(1024))) char ring0[(XT + YT) * kStageBytes], ring1[(XT + YT) * kStageBytes],
-            ring2[(XT + YT) * kStageBytes], ring3[(XT + YT) * kStageBytes];
-        __shared__ __attribute__((aligned(16))) uint8_t scales0[Mul::kScaled ? kScaleBytes : 16], scales1[Mul::kScaled ? kScaleBytes : 16];
-        typedef StageLoads<XT, XS, kThreads> LoadsX;
-        typedef StageLoads<YT, YS, kThreads> LoadsY;
+        __shared__ __attribute__((aligned(1024))) char ring0[(XT + YT) * kStepBytes * H], ring1[(XT + YT) * kStepBytes * H],
+            ring2[(XT + YT) * kStepBytes * H], ring3[(XT + YT) * kStepBytes * H];
+        __shared__ __attribute__((aligned(16))) uint8_t scales0[Mul::kScaled ? kScaleBytes * H : 16], scales1[Mul::kScaled ? kScaleBytes * H : 16];
+        typedef StageLoads<XT, XS, kThreads, H> LoadsX;
+        typedef StageLoads<YT, YS, kThreads, H> LoadsY;
         LoadsX lx;
         LoadsY ly;
         lx.init(x);
@@ -300,14 +330,14 @@ struct TileProduct {
         for (int m = 0; m < SX; ++m)
 #pragma unroll
             for (int n = 0; n < SY; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int per = static_cast<int>((k1 - k0) / 32), stages = PARTS ? per * kPartSteps : per;
+        const int per = static_cast<int>((k1 - k0 + 32 * H - 1) / (32 * H)), stages = PARTS ? per * kPartSteps : per;
         if (stages <= 0) return;
-        address_x = part_address<XT, XS>(sub_x(0));
-        address_y = part_address<YT, YS>(sub_y(0));
-        const Reader<XT, XS> bx(x, i0, k0);
-        const Reader<YT, YS> by(y, j0, k0);
-        Reader<XT, XS> rx = bx;
-        Reader<YT, YS> ry = by;
+        address_x = part_address<XT, XS, H>(sub_x(0));
+        address_y = part_address<YT, YS, H>(sub_y(0));
+        const Reader<XT, XS, H> bx(x, i0, k0);
+        const Reader<YT, YS, H> by(y, j0, k0);
+        Reader<XT, XS, H> rx = bx;
+        Reader<YT, YS, H> ry = by;
         int coming = stages, at = per, part = 0;     // stages to be loaded yet, of this product of parts
         auto select = [&] {
             rx = bx;
@@ -316,71 +346,77 @@ struct TileProduct {
             ry.p += ((kPartsY >> (2 * part)) & 3) * y.plane;
         };
         if constexpr (PARTS) select();
-        // Loads of a stage in kSteps parts.  Behind the last stage they find nothing and bring zeros, so that every wavefront has as
-        // many loads under way as ever.
+        // Loads of a stage, asked for in kSlices slices.  Behind the last stage they find nothing and bring zeros, so that every wavefront
+        // has as many loads under way as ever.
+        constexpr int kSlices = kParts > 1 ? 2 : 1;
         const int to = wave() * kWave * 16;
-        auto load = [&](char *ring, int step) {
-            lx.issue(rx.buffer(coming > 0), ring, to, step, kSteps);
-            ly.issue(ry.buffer(coming > 0), ring, kY + to, step, kSteps);
-            if (step + 1 < kSteps) return;
+        auto load = [&](char *ring, int slice) {
+            const int wide = static_cast<int>(k1 - k0) * 2 - (per - at) * kStepBytes * H;
+            lx.issue(rx.buffer(coming > 0), ring, to, slice, kSlices, wide);
+            ly.issue(ry.buffer(coming > 0), ring, kY + to, slice, kSlices, wide);
+            if (slice + 1 < kSlices) return;
             --coming;
             rx.next();
             ry.next();
+            if (PARTS || H > 1) --at;
             if constexpr (PARTS)
-                if (--at == 0) {
+                if (at == 0) {
                     at = per;
                     ++part;
                     select();
                 }
         };
-        i32x4 px[2][kQ], py[2][SY];             // of a step and of the next: x by the step, y by the stage
+        static_assert(H == 1 || H * kPer % 2 == 0, "parity");
+        i32x4 px[2][kQ], py[2][SY];             // of a part and of the next: x by the part, y by the step
         Scales scales{}, scales_next{};
-        uint32_t brought[2] = {};               // scales on their way to LDS, by the stage
+        Brought brought[2] = {};                // scales on their way to LDS, by the stage
         const uint8_t *row = nullptr;
         const int64_t groups = k1 / 32;
         if constexpr (Mul::kScaled) {
             const int t = threadIdx.x;
             row = t < XT ? x.scales + lesser(i0 + t, x.rows - 1) * x.ld_scales : t < XT + YT ? y.scales + lesser(j0 + t - XT, y.rows - 1) * y.ld_scales : nullptr;
-            write_scales(scales0, load_scales(row, k0 / 32, groups));
-            write_scales(scales1, load_scales(row, k0 / 32 + 1, groups));
-            brought[0] = load_scales(row, k0 / 32 + 2, groups);
-            brought[1] = load_scales(row, k0 / 32 + 3, groups);
+            write_scales(scales0, load_scales(row, 0, groups));
+            write_scales(scales1, load_scales(row, 1, groups));
+            brought[0] = load_scales(row, 2, groups);
+            brought[1] = load_scales(row, 3, groups);
         }
         auto load_all = [&](char *ring) {
 #pragma unroll
-            for (int step = 0; step < kSteps; ++step) load(ring, step);
+            for (int slice = 0; slice < kSlices; ++slice) load(ring, slice);
         };
         load_all(ring0);
         load_all(ring1);
         load_all(ring2);
-        if (kSteps > 1) load(ring3, 0);
-        constexpr int kEach = LoadsX::kSurely + LoadsY::kSurely, kFirst = kSteps > 1 ? kEach / 2 : 0;
+        if (kSlices > 1) load(ring3, 0);
+        // loads that every wavefront has under way per stage, of a first slice
+        constexpr int kEach = LoadsX::kSurely + LoadsY::kSurely, kFirst = kSlices > 1 ? LoadsX::first(kSlices) + LoadsY::first(kSlices) : 0;
         stage_arrived<2 * kEach + kFirst>();
-        read_step(ring0, 0, px[0], py[0]);
+        read_part(ring0, 0, px[0], py[0]);
         if constexpr (Mul::kScaled) read_scales(scales0, scales);
-        // Stage s out of `now`; `next` holds the next one, the second part of `later` is still to be asked for.
+        // Stage s out of `now`; `next` holds the next one, the second slice of `later` is still to be asked for.
         auto stage = [&](char *now, char *next, char *later, uint8_t *ss, uint8_t *sn, int parity, int s) {
+            constexpr int kPerX = XS ? 2 : 1, kPerY = YS ? 2 : 1;
 #pragma unroll
-            for (int step = 0; step < kSteps; ++step) {
+            for (int part = 0; part < kParts; ++part) {
                 __builtin_amdgcn_sched_barrier(0);
-                constexpr int kPerX = XS ? 2 : 1, kPerY = YS ? 2 : 1;
-                const int mine = kSteps == 1 ? parity : step & 1, coming = mine ^ 1;
-                if (step + 1 < kSteps) {
-                    read_step(now, step + 1, px[coming], py[parity]);
-                    load(later, step + 1);
+                const int mine = (kParts & 1 ? parity : 0) ^ (part & 1), yours = (H & 1 ? parity : 0) ^ (part / kPer & 1);
+                const int y_next = (part + 1) % kPer ? yours : yours ^ 1;
+                if (part + 1 < kParts) {
+                    read_part(now, part + 1, px[mine ^ 1], py[y_next]);
+                    if (part == 0) load(later, 1);
                 } else {
-                    stage_arrived<(kSteps == 1 ? 1 : 2) * kEach>();      // the next stage's; what was asked for since then is on its way
+                    stage_arrived<(kSlices > 1 ? 2 : 1) * kEach>();      // the next stage's; what was asked for since then is on its way
                     if constexpr (Mul::kScaled) {
                         read_scales(sn, scales_next);                    // written before this barrier
                         write_scales(ss, brought[parity]);               // stage s + 2's; what was there was read before it
-                        brought[parity] = load_scales(row, k0 / 32 + s + 4, groups);
+                        brought[parity] = load_scales(row, s + 4, groups);
                     }
-                    read_step(next, 0, px[coming], py[parity ^ 1]);    // (after the last stage: zeros)
-                    load(kSteps == 1 ? later : now, 0);
+                    read_part(next, 0, px[mine ^ 1], py[y_next]);        // (after the last stage: zeros)
+                    load(kSlices > 1 ? now : later, 0);
                 }
-                multiply_step(px[mine], py[parity], step, scales);
-                if (step + 1 < kSteps) order_step<kQ * kPerX, kQ * SY>();
-                else order_step<kQ * kPerX + SY * kPerY, kQ * SY>();
+                multiply_part(px[mine], py[yours], part, scales);
+                if ((part + 1) % kPer) order_part<kQ * kPerX, kQ * SY>();
+                else order_part<kQ * kPerX + SY * kPerY, kQ * SY>();
             }
             if constexpr (Mul::kScaled) scales = scales_next;
         };
@@ -457,6 +493,25 @@ __device__ __forceinline__ void tile_of_block(int block, int tiles_x, int tiles_
     const int span = kGroup * tiles_x, group = t / span, first = group * kGroup, high = min(kGroup, tiles_y - first), in = t % span;
     ty = first + in % high;
     tx = in / high;
+}
+
+// Tiles of the products.  What a tile's side costs in the efficiency of the matrix cores it gains where there are few tiles: measured on
+// large products 256 x 256 reaches 1170 to 1330 TFLOP/s, 128 x 128 820 to 1120; 8192 rows of the smaller one's blocks, two to a compute
+// unit, take 1.4 times as long as the larger's for the same work.
+enum TileSize { kTile256, kTile128, kTile64, kTile16 };      // the last: 16 rows by 64 (classes) or 128 (columns)
+
+constexpr int side(TileSize s) { return s == kTile256 ? 256 : s == kTile128 ? 128 : s == kTile64 ? 64 : 16; }
+
+// The larger tile, unless the rounds its blocks take on 256 compute units are so much emptier than the smaller's that those are faster.
+inline TileSize tile_for(int64_t x, int64_t y)
+{
+    const int64_t big = (x + 255) / 256 * ((y + 255) / 256), small = (x + 127) / 128 * ((y + 127) / 128);
+    return 1.4 * 0.5 * static_cast<double>((small + 511) / 512) < static_cast<double>((big + 255) / 256) ? kTile128 : kTile256;
+}
+// ... of products over `rows` rows.
+inline TileSize tile_for_rows(int64_t x, int64_t rows)
+{
+    return rows <= 16 ? kTile16 : rows <= 64 ? kTile64 : tile_for(x, rows);
 }
 
 }  // namespace dq

@@ -106,11 +106,11 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__re
     }
 }
 
-template <int TYPE, int XT, int YT, int WX, int WY>
+template <int TYPE, int XT, int YT, int WX, int WY, int H>
 __global__ __launch_bounds__(WX *WY *kWave) void mx4_product_kernel(Operand w, Operand a, int64_t k, int tiles_x, int tiles_y,
                                                                     typename Num<TYPE>::Mem *__restrict__ out, int64_t ld, int vector)
 {
-    typedef TileProduct<MulMx4, XT, YT, WX, WY, false, false> Tile;
+    typedef TileProduct<MulMx4, XT, YT, WX, WY, false, false, H> Tile;
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t i0 = static_cast<int64_t>(tx) * XT, j0 = static_cast<int64_t>(ty) * YT;
@@ -168,14 +168,13 @@ static int32_t quantize4(const void *v, int32_t type, int64_t ld, const dq_mx4 &
     }
 }
 
-template <int TYPE, int YT, int WX, int WY>
+template <int TYPE, int kXT, int YT, int WX, int WY, int H>
 static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int64_t ld, hipStream_t st)
 {
-    constexpr int kXT = 256;
     const int64_t tiles_x = (w.n + kXT - 1) / kXT, tiles_y = (a.n + YT - 1) / YT;
     if (tiles_x * tiles_y > kMost4) return DQ_ERR_UNSUPPORTED;
     auto operand = [](const dq_mx4 &q) { return Operand{reinterpret_cast<const char *>(q.codes), q.ld_codes, q.n, static_cast<int32_t>(groups_of(q.d) * 32), 0, q.scales, q.ld_scales}; };
-    mx4_product_kernel<TYPE, kXT, YT, WX, WY><<<static_cast<unsigned>(tiles_x * tiles_y), WX * WY * kWave, 0, st>>>(
+    mx4_product_kernel<TYPE, kXT, YT, WX, WY, H><<<static_cast<unsigned>(tiles_x * tiles_y), WX * WY * kWave, 0, st>>>(
         operand(w), operand(a), groups_of(a.d) * 32, static_cast<int>(tiles_x), static_cast<int>(tiles_y), static_cast<typename Num<TYPE>::Mem *>(out), ld,
         four_at_once(out, ld, wide_of(TYPE)));
     DQ_LAUNCH_CHECK();
@@ -184,9 +183,12 @@ static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int64_t ld,
 template <int TYPE>
 static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int64_t ld, hipStream_t st)
 {
-    if (a.n <= 16) return product4<TYPE, 16, 8, 1>(a, w, out, ld, st);
-    if (a.n <= 64) return product4<TYPE, 64, 4, 2>(a, w, out, ld, st);
-    return product4<TYPE, 256, 2, 4>(a, w, out, ld, st);
+    switch (tile_for_rows(w.n, a.n)) {
+    case kTile256: return product4<TYPE, 256, 256, 2, 4, 1>(a, w, out, ld, st);
+    case kTile128: return product4<TYPE, 128, 128, 2, 2, 1>(a, w, out, ld, st);
+    case kTile64: return product4<TYPE, 64, 64, 2, 2, 2>(a, w, out, ld, st);
+    default: return product4<TYPE, 64, 16, 4, 1, 2>(a, w, out, ld, st);
+    }
 }
 static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int32_t type, int64_t ld, hipStream_t st)
 {
