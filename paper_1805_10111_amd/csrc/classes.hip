@@ -366,26 +366,26 @@ __global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand 
             }
         }
 #pragma unroll
-        for (int m = 0; m < Tile::SX; ++m) {
-            u16 part[3][4];
+        for (int m = 0; m < Tile::SX; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float v = live && base + 16 * m + i < c ? f * tile.acc[m][y][i] : 0.0f;
-                if constexpr (TYPE == DQ_F32) {
-                    u16 p[3];
-                    parts_of(v, p);
-                    part[0][i] = p[0];
-                    part[1][i] = p[1];
-                    part[2][i] = p[2];
-                } else {
-                    part[0][i] = Num<TYPE>::store(v);
+            for (int i = 0; i < 4; ++i) tile.acc[m][y][i] = live && base + 16 * m + i < c ? f * tile.acc[m][y][i] : 0.0f;
+    }
+    u16 *const to = g + t0 * ldg + (c0 - piece0);
+    if constexpr (TYPE == DQ_F32) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p)                // (each part is taken off before the next is)
+            tile.store(to + p * plane, ldg, YT, XT, [&](int m, int n) {
+                u16x4 r;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float v = tile.acc[m][n][i];
+                    r[i] = Part::store(v);
+                    tile.acc[m][n][i] = __builtin_isfinite(Part::load(r[i])) ? v - Part::load(r[i]) : 0.0f;
                 }
-            }
-            u16 *const to = g + t * ldg + (base + 16 * m - piece0);
-#pragma unroll
-            for (int p = 0; p < (TYPE == DQ_F32 ? 3 : 1); ++p)
-                *reinterpret_cast<u16x4 *>(to + p * plane) = u16x4{part[p][0], part[p][1], part[p][2], part[p][3]};
-        }
+                return r;
+            });
+    } else {
+        tile.store(to, ldg, YT, XT, [&](int m, int n) { return quad_of<TYPE>(tile.acc[m][n]); });
     }
 }
 
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(256) void da_finish_kernel(const float *__restrict_
 template <int TYPE, int XT, int YT, int WX, int WY, int H>
 __global__ __launch_bounds__(WX *WY *kWave) void dw_kernel(Operand a, Operand g, int64_t k, int64_t piece, int64_t d, int tiles_x, int tiles_y,
                                                            float post, const float *__restrict__ weight_max,
-                                                           typename Num<TYPE>::Mem *__restrict__ dw, int64_t lddw, int vector)
+                                                           typename Num<TYPE>::Mem *__restrict__ dw, int64_t lddw)
 {
     typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, true, H> Tile;
     int tx, ty;
@@ -462,16 +462,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void dw_kernel(Operand a, Operand g,
     Tile tile;
     tile.template run<TYPE == DQ_F32>(a, g, i0, j0, 0, k);
     const float unit = gradient_unit(TYPE, post, weight_max);
-#pragma unroll
-    for (int y = 0; y < Tile::SY; ++y) {
-        const int64_t j = j0 + Tile::at_y(y);
-        if (j >= piece) continue;
-#pragma unroll
-        for (int m = 0; m < Tile::SX; ++m) {
-            const int64_t i = i0 + Tile::at_x(m);
-            if (i < d) store_four<TYPE>(dw + j * lddw + i, tile.acc[m][y] * unit, static_cast<int>(lesser(4, d - i)), vector);
-        }
-    }
+    tile.store(dw + j0 * lddw + i0, lddw, piece - j0, d - i0, [&](int m, int n) { return quad_of<TYPE>(tile.acc[m][n] * unit); });
 }
 
 // ---- host ----------------------------------------------------------------------
@@ -661,7 +652,7 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     float *const partial = s.da_at_once ? nullptr : reinterpret_cast<float *>(ws + s.partial);
     const int64_t plane = s.rows_g * s.ldg;
     const Operand go{reinterpret_cast<const char *>(g), s.ldg * 2, s.rows_g, static_cast<int32_t>(s.ldg), plane * 2};
-    const int vector_da = four_at_once(q.da, q.ldda, static_cast<int>(wide)), vector_dw = four_at_once(q.dw, q.lddw, static_cast<int>(wide));
+    const int vector_da = four_at_once(q.da, q.ldda, static_cast<int>(wide));
     Mem *const da = static_cast<Mem *>(q.da);
     for (int64_t at = 0; at < c; at += s.piece) {
         const int64_t have = std::min(s.piece, c - at);
@@ -677,7 +668,7 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
         if (q.dw) {
             const int t = side(s.tile_dw), tx = static_cast<int>((s.d + t - 1) / t), ty = static_cast<int>((have + t - 1) / t);
             DQ_TILE_LAUNCH(s.tile_dw, dw_kernel, (dw_kernel<TYPE, 64, 64, 2, 2, 2>), static_cast<unsigned>(tx * ty), az, go, s.rows_z, have, s.d, tx, ty, post, weight_max,
-                           static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw, vector_dw);
+                           static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw);
         }
     }
     if (q.da && partial) {

@@ -170,7 +170,14 @@ struct Reader {
             left = static_cast<int32_t>((lesser(o.rows - i0, T) - 1) * o.ld + 2 * (o.cols - k0));
             edge = 0;
         }
+        // (the same in every lane, which the compiler does not see everywhere: it would go through the lanes in a loop at each load)
+        const uint64_t at = reinterpret_cast<uint64_t>(p);
+        p = reinterpret_cast<const char *>(static_cast<uint64_t>(same(static_cast<int>(at >> 32))) << 32 | static_cast<uint32_t>(same(static_cast<int>(at))));
+        left = same(left);
+        ld = same(ld);
+        edge = same(edge);
     }
+    static __device__ __forceinline__ int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
     // any: whether there is another stage
     __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(bool any) const
     {
@@ -312,13 +319,68 @@ struct TileProduct {
         __builtin_amdgcn_sched_group_barrier(kMatrix, PRODUCTS, 0);
     }
 
+    static constexpr int kRingBytes = (XT + YT) * kStepBytes * H;
+    // the first stage's memory; the results pass through it
+    static __device__ __forceinline__ char *first_ring()
+    {
+        __shared__ __attribute__((aligned(1024))) char ring0[kRingBytes];
+        return ring0;
+    }
+
+    // Stores the tile row by row j, value(m, n) the four results of subtile (m, n) in memory's type: out: where the tile's first row
+    // begins, rows, cols: how many of the tile's rows and of their columns there are.  A lane's four results are 8 or 16 bytes of one of sixteen
+    // rows; each wavefront turns them, through its part of LDS, into up to 256 neighbouring bytes of a row.  (Scores of 8192 x 47236
+    // classes: written four at a time 1290 us, so ___ us.)
+    template <class Mem, class Value>
+    __device__ __forceinline__ void store(Mem *out, int64_t ld, int64_t rows, int64_t cols, Value value) const
+    {
+        typedef __attribute__((ext_vector_type(4))) Mem Quad;
+        struct __attribute__((packed, aligned(sizeof(Mem)))) Chunk {
+            i32x4 v;
+        };
+        constexpr int kSize = sizeof(Mem), kCols = SX * 16 < 256 / kSize ? SX * 16 : 256 / kSize, kSub = kCols / 16, kCh = kCols * kSize / 16;
+        constexpr int kEach = 16 / kSize;                         // numbers of a chunk
+        static_assert(16 * kCols * kSize * WX * WY <= kRingBytes, "a part of the first stage for each wavefront");
+        __syncthreads();
+        char *const mine = first_ring() + wave() * 16 * kCols * kSize;
+        const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int n = 0; n < SY; ++n)
+#pragma unroll
+            for (int group = 0; group < SX / kSub; ++group) {
+#pragma unroll
+                for (int m = 0; m < kSub; ++m) {
+                    const int at = (m * 16 + g * 4) * kSize, chunk = at / 16 ^ (j & (kCh - 1));
+                    *reinterpret_cast<Quad *>(mine + j * kCols * kSize + chunk * 16 + at % 16) = value(group * kSub + m, n);
+                }
+#pragma unroll
+                for (int i = 0; i < (16 * kCh + 63) / 64; ++i) {
+                    const int id = i * 64 + lane, r = id / kCh, chunk = id % kCh;
+                    if (16 * kCh < 64 && r >= 16) continue;
+                    const i32x4 v = *reinterpret_cast<const i32x4 *>(mine + r * kCols * kSize + (chunk ^ (r & (kCh - 1))) * 16);
+                    const int64_t row = sub_y(n) * 16 + r, col = sub_x(group * kSub) * 16 + chunk * kEach;
+                    if (row >= rows || col >= cols) continue;
+                    Mem *const to = out + row * ld + col;
+                    if (col + kEach <= cols) {
+                        reinterpret_cast<Chunk *>(to)->v = v;
+                    } else {
+                        typedef __attribute__((ext_vector_type(kEach))) Mem All;
+                        const All each = __builtin_bit_cast(All, v);
+#pragma unroll
+                        for (int e = 0; e < kEach; ++e)
+                            if (col + e < cols) to[e] = each[e];
+                    }
+                }
+            }
+    }
+
     // k0 .. k1 (in pairs of bytes, multiples of 32) of rows i0.. of x and j0.. of y.  PARTS: operands are float32 in parts.
     template <bool PARTS>
     __device__ __forceinline__ void run(const Operand &x, const Operand &y, int64_t i0, int64_t j0, int64_t k0, int64_t k1)
     {
         // (an array of its own for each stage: the compiler keeps apart what is read and what is arriving by the array, up to seven)
-        __shared__ __attribute__((aligned(1024))) char ring0[(XT + YT) * kStepBytes * H], ring1[(XT + YT) * kStepBytes * H],
-            ring2[(XT + YT) * kStepBytes * H], ring3[(XT + YT) * kStepBytes * H];
+        __shared__ __attribute__((aligned(1024))) char ring1[kRingBytes], ring2[kRingBytes], ring3[kRingBytes];
+        char *const ring0 = first_ring();
         __shared__ __attribute__((aligned(16))) uint8_t scales0[Mul::kScaled ? kScaleBytes * H : 16], scales1[Mul::kScaled ? kScaleBytes * H : 16];
         typedef StageLoads<XT, XS, kThreads, H> LoadsX;
         typedef StageLoads<YT, YS, kThreads, H> LoadsY;
@@ -369,14 +431,14 @@ struct TileProduct {
         static_assert(H == 1 || H * kPer % 2 == 0, "parity");
         i32x4 px[2][kQ], py[2][SY];             // of a part and of the next: x by the part, y by the step
         Scales scales{}, scales_next{};
-        Brought brought[2] = {};                // scales on their way to LDS, by the stage
+        Brought brought[2] = {}, scales_at[2] = {};      // scales on their way to LDS, by the stage; of the first two stages
         const uint8_t *row = nullptr;
         const int64_t groups = k1 / 32;
         if constexpr (Mul::kScaled) {
             const int t = threadIdx.x;
             row = t < XT ? x.scales + lesser(i0 + t, x.rows - 1) * x.ld_scales : t < XT + YT ? y.scales + lesser(j0 + t - XT, y.rows - 1) * y.ld_scales : nullptr;
-            write_scales(scales0, load_scales(row, 0, groups));
-            write_scales(scales1, load_scales(row, 1, groups));
+            scales_at[0] = load_scales(row, 0, groups);
+            scales_at[1] = load_scales(row, 1, groups);
             brought[0] = load_scales(row, 2, groups);
             brought[1] = load_scales(row, 3, groups);
         }
@@ -388,6 +450,10 @@ struct TileProduct {
         load_all(ring1);
         load_all(ring2);
         if (kSlices > 1) load(ring3, 0);
+        if constexpr (Mul::kScaled) {
+            write_scales(scales0, scales_at[0]);
+            write_scales(scales1, scales_at[1]);
+        }
         // loads that every wavefront has under way per stage, of a first slice
         constexpr int kEach = LoadsX::kSurely + LoadsY::kSurely, kFirst = kSlices > 1 ? LoadsX::first(kSlices) + LoadsY::first(kSlices) : 0;
         stage_arrived<2 * kEach + kFirst>();
@@ -461,6 +527,14 @@ struct Num<DQ_BF16> {
     static __device__ __forceinline__ Mem store(float v) { return __builtin_bit_cast(u16, static_cast<__bf16>(v)); }
 };
 typedef Num<DQ_BF16> Part;                       // of a float32
+
+template <int TYPE>
+using Quad = __attribute__((ext_vector_type(4))) typename Num<TYPE>::Mem;
+template <int TYPE>
+__device__ __forceinline__ Quad<TYPE> quad_of(f32x4 v)
+{
+    return Quad<TYPE>{Num<TYPE>::store(v[0]), Num<TYPE>::store(v[1]), Num<TYPE>::store(v[2]), Num<TYPE>::store(v[3])};
+}
 
 // Four neighbouring results of one row.
 template <int TYPE>

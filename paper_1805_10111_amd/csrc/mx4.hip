@@ -108,7 +108,7 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__re
 
 template <int TYPE, int XT, int YT, int WX, int WY, int H>
 __global__ __launch_bounds__(WX *WY *kWave) void mx4_product_kernel(Operand w, Operand a, int64_t k, int tiles_x, int tiles_y,
-                                                                    typename Num<TYPE>::Mem *__restrict__ out, int64_t ld, int vector)
+                                                                    typename Num<TYPE>::Mem *__restrict__ out, int64_t ld)
 {
     typedef TileProduct<MulMx4, XT, YT, WX, WY, false, false, H> Tile;
     int tx, ty;
@@ -116,16 +116,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void mx4_product_kernel(Operand w, O
     const int64_t i0 = static_cast<int64_t>(tx) * XT, j0 = static_cast<int64_t>(ty) * YT;
     Tile tile;
     tile.template run<false>(w, a, i0, j0, 0, k);
-#pragma unroll
-    for (int y = 0; y < Tile::SY; ++y) {
-        const int64_t j = j0 + Tile::at_y(y);
-        if (j >= a.rows) continue;
-#pragma unroll
-        for (int m = 0; m < Tile::SX; ++m) {
-            const int64_t i = i0 + Tile::at_x(m);
-            if (i < w.rows) store_four<TYPE>(out + j * ld + i, tile.acc[m][y], static_cast<int>(lesser(4, w.rows - i)), vector);
-        }
-    }
+    tile.store(out + j0 * ld + i0, ld, a.rows - j0, w.rows - i0, [&](int m, int n) { return quad_of<TYPE>(tile.acc[m][n]); });
 }
 
 // ---- host ----------------------------------------------------------------------
@@ -175,8 +166,7 @@ static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int64_t ld,
     if (tiles_x * tiles_y > kMost4) return DQ_ERR_UNSUPPORTED;
     auto operand = [](const dq_mx4 &q) { return Operand{reinterpret_cast<const char *>(q.codes), q.ld_codes, q.n, static_cast<int32_t>(groups_of(q.d) * 32), 0, q.scales, q.ld_scales}; };
     mx4_product_kernel<TYPE, kXT, YT, WX, WY, H><<<static_cast<unsigned>(tiles_x * tiles_y), WX * WY * kWave, 0, st>>>(
-        operand(w), operand(a), groups_of(a.d) * 32, static_cast<int>(tiles_x), static_cast<int>(tiles_y), static_cast<typename Num<TYPE>::Mem *>(out), ld,
-        four_at_once(out, ld, wide_of(TYPE)));
+        operand(w), operand(a), groups_of(a.d) * 32, static_cast<int>(tiles_x), static_cast<int>(tiles_y), static_cast<typename Num<TYPE>::Mem *>(out), ld);
     DQ_LAUNCH_CHECK();
     return DQ_OK;
 }
