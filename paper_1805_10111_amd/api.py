@@ -443,11 +443,12 @@ TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 def _matrix(t: torch.Tensor, name: str, dtype=None, shape=None):
     """(pointer, row stride) of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    size = t.shape
+    if len(size) != 2 or (size[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be a matrix with contiguous rows")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    return _ptr(t, dtype, name), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    if shape is not None and size != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(size)}")
+    return _ptr(t, dtype, name), t.stride(0) if size[0] > 1 else max(t.stride(0), size[1])
 
 
 def _vector(t: Optional[torch.Tensor], dtype, name: str, n: int):
@@ -574,8 +575,9 @@ class Mx4:
     def __post_init__(self):
         s = _Mx4()
         n = self.codes.shape[0]
-        s.codes, s.ld_codes = _matrix(self.codes, "codes", torch.uint8, (n, dq_mx4_row_bytes(self.d)))
-        s.scales, s.ld_scales = _matrix(self.scales, "scales", torch.uint8, (n, dq_mx4_row_scales(self.d)))
+        groups = (self.d + 127) // 128
+        s.codes, s.ld_codes = _matrix(self.codes, "codes", torch.uint8, (n, 64 * groups))
+        s.scales, s.ld_scales = _matrix(self.scales, "scales", torch.uint8, (n, 4 * groups))
         s.n, s.d = n, self.d
         self._s = s
 
@@ -590,8 +592,9 @@ class Mx4:
 
 def new_mx4(n: int, d: int, device="cuda") -> Mx4:
     """Room for an [n, d] matrix in 4 bits (not initialised)."""
-    u8 = dict(dtype=torch.uint8, device=device)
-    return Mx4(torch.empty((n, dq_mx4_row_bytes(d)), **u8), torch.empty((n, dq_mx4_row_scales(d)), **u8), d)
+    groups = (d + 127) // 128                                   # codes and scales side by side: one allocation
+    room = torch.empty(n * 68 * groups, dtype=torch.uint8, device=device)
+    return Mx4(room[:n * 64 * groups].view(n, 64 * groups), room[n * 64 * groups:].view(n, 4 * groups), d)
 
 
 def _typed(t: torch.Tensor, name: str, shape):

@@ -7,6 +7,8 @@
 
 namespace dq {
 
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+
 constexpr int kGroup4 = 128;                   // numbers of a row that are stored together: 64 bytes of codes, 4 scales
 
 __host__ __device__ static inline int64_t groups_of(int64_t d) { return (d + kGroup4 - 1) / kGroup4; }
@@ -20,20 +22,18 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits)
 }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
 
-// Eight numbers of a row from column c on, zeros behind its end.
+// Eight numbers of a row from column c on, zeros behind its end.  (16-byte loads of any alignment to the number.)
 template <int TYPE>
-__device__ __forceinline__ void load_eight(const typename Num<TYPE>::Mem *row, int64_t c, int64_t d, bool vector, float out[8])
+__device__ __forceinline__ void load_eight(const typename Num<TYPE>::Mem *row, uint32_t c, uint32_t d, float out[8])
 {
     typedef typename Num<TYPE>::Mem Mem;
-    typedef __attribute__((ext_vector_type(16 / sizeof(Mem)))) Mem Wide;
-    constexpr int kPer = 16 / sizeof(Mem);
-    if (vector && c + 8 <= d) {
+    if (c + 8 <= d) {
+        struct __attribute__((packed, aligned(sizeof(Mem)))) All {
+            __attribute__((ext_vector_type(8))) Mem v;
+        };
+        const All all = *reinterpret_cast<const All *>(row + c);
 #pragma unroll
-        for (int h = 0; h < 8 / kPer; ++h) {
-            const Wide v = *reinterpret_cast<const Wide *>(row + c + h * kPer);
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) out[h * kPer + e] = Num<TYPE>::load(v[e]);
-        }
+        for (int e = 0; e < 8; ++e) out[e] = Num<TYPE>::load(all.v[e]);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) out[e] = c + e < d ? Num<TYPE>::load(row[c + e]) : 0.0f;
@@ -59,50 +59,91 @@ __device__ __forceinline__ uint32_t quantize_eight(const float v[8], uint32_t &b
     return code;
 }
 
-// A thread takes eight numbers: 16 or 32 bytes read, 4 written; four neighbouring lanes share a block.
+// Item i of rows of `per` items: its row and place there.  (Rows and items are numbered in 32 bits; where a matrix has more items, in several
+// launches' worth of blocks by blockIdx.y.)
+struct Place {
+    int64_t row;
+    uint32_t at;
+};
+__device__ __forceinline__ Place place_of(uint32_t i, uint32_t per, int64_t row0)
+{
+    const uint32_t r = i / per;
+    return Place{row0 + r, i - r * per};
+}
+
+// A thread takes eight numbers: 16 or 32 bytes read, 4 written; four neighbouring lanes share a block.  What bounds it is memory:
+// 47236 x 4096 in bfloat16 (490 MB) 94 us, in float32 (877 MB) 154 us; two and four items a thread 90 to 95 and 97 to 100, 160 and 169.
 template <int TYPE>
-__global__ __launch_bounds__(256) void mx4_quantize_kernel(const typename Num<TYPE>::Mem *__restrict__ v, int64_t n, int64_t d, int64_t ld, int vector,
+__global__ __launch_bounds__(256) void mx4_quantize_kernel(const typename Num<TYPE>::Mem *__restrict__ v, int64_t n, int64_t rows, uint32_t d, int64_t ld,
                                                            uint8_t *__restrict__ codes, int64_t ld_codes, uint8_t *__restrict__ scales,
                                                            int64_t ld_scales, uint32_t *__restrict__ status)
 {
-    const int64_t per = groups_of(d) * 16, total = n * per;             // a multiple of four: a block's lanes stay together
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
-        const int64_t r = i / per, at = i - r * per;
-        float x[8];
-        load_eight<TYPE>(v + r * ld, at * 8, d, vector, x);
-        uint32_t byte;
-        const uint32_t code = quantize_eight(x, byte);
-        *reinterpret_cast<uint32_t *>(codes + r * ld_codes + at * 4) = code;
-        if ((at & 3) == 0) {
-            scales[r * ld_scales + at / 4] = static_cast<uint8_t>(byte);
-            if (byte == 255 && status) atomicOr(status, 1u);
-        }
+    const int64_t row0 = blockIdx.y * rows;
+    const uint32_t per = (d + kGroup4 - 1) / kGroup4 * 16, total = static_cast<uint32_t>(lesser(rows, n - row0)) * per;
+    const uint32_t i = blockIdx.x * 256u + threadIdx.x;             // per is a multiple of four: a block's lanes stay together
+    if (i >= total) return;
+    const Place p = place_of(i, per, row0);
+    float x[8];
+    load_eight<TYPE>(v + p.row * ld, p.at * 8, d, x);
+    uint32_t byte;
+    const uint32_t code = quantize_eight(x, byte);
+    *reinterpret_cast<uint32_t *>(codes + p.row * ld_codes + p.at * 4) = code;
+    if ((p.at & 3) == 0) {
+        scales[p.row * ld_scales + p.at / 4] = static_cast<uint8_t>(byte);
+        if (byte == 255 && status) atomicOr(status, 1u);
     }
 }
 
+// Eight values of a row.
 template <int TYPE>
-__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes, int64_t ld_codes, const uint8_t *__restrict__ scales,
-                                                             int64_t ld_scales, int64_t n, int64_t d, typename Num<TYPE>::Mem *__restrict__ out,
-                                                             int64_t ld, int vector)
+__device__ __forceinline__ void store_eight(typename Num<TYPE>::Mem *to, const float v[8], int have)
 {
-    const int64_t per = (d + 7) / 8, total = n * per;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
-        const int64_t r = i / per, at = i - r * per;
-        const uint32_t code = *reinterpret_cast<const uint32_t *>(codes + r * ld_codes + at * 4);
-        const int byte = scales[r * ld_scales + at / 4];
-        f32x4 x[2];
+    typedef typename Num<TYPE>::Mem Mem;
+    struct __attribute__((packed, aligned(sizeof(Mem)))) All {
+        __attribute__((ext_vector_type(8))) Mem v;
+    } all;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t c = (code >> (4 * e)) & 7u;
-            // level = (1 + m / 2) 2^(x - 1), below 1 m / 2
-            const float level = c < 2 ? 0.5f * static_cast<float>(c) : __uint_as_float(((c >> 1) + 126u) << 23 | (c & 1u) << 22);
-            const float value = ldexpf(level, byte - 127);
-            x[e >> 2][e & 3] = byte == 255 ? __uint_as_float(0x7fc00000u) : (code >> (4 * e)) & 8u ? -value : value;
-        }
-        const int have = static_cast<int>(lesser(8, d - at * 8));
-        typename Num<TYPE>::Mem *const to = out + r * ld + at * 8;
-        store_four<TYPE>(to, x[0], min(have, 4), vector);
-        if (have > 4) store_four<TYPE>(to + 4, x[1], have - 4, vector);
+    for (int e = 0; e < 8; ++e) all.v[e] = Num<TYPE>::store(v[e]);
+    if (have >= 8) {
+        *reinterpret_cast<All *>(to) = all;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < have) to[e] = all.v[e];
+    }
+}
+
+// The inverse, AT_ONCE items a thread requested together.  47236 x 4096 to bfloat16 (490 MB): one 107 us, two 98, four 88; to float32
+// (877 MB) 172, 220 and 228: there the stores are twice as long, and one it is.
+template <int TYPE, int AT_ONCE>
+__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes, int64_t ld_codes, const uint8_t *__restrict__ scales,
+                                                             int64_t ld_scales, int64_t n, int64_t rows, uint32_t d, typename Num<TYPE>::Mem *__restrict__ out,
+                                                             int64_t ld)
+{
+    const int64_t row0 = blockIdx.y * rows;
+    const uint32_t per = (d + 7) / 8, total = static_cast<uint32_t>(lesser(rows, n - row0)) * per, first = blockIdx.x * (256u * AT_ONCE) + threadIdx.x;
+    uint32_t code[AT_ONCE] = {};
+    int byte[AT_ONCE] = {};
+    Place p[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+        const uint32_t i = first + 256u * u;
+        p[u] = place_of(i, per, row0);
+        if (i >= total) continue;
+        code[u] = *reinterpret_cast<const uint32_t *>(codes + p[u].row * ld_codes + p[u].at * 4);
+        byte[u] = scales[p[u].row * ld_scales + p[u].at / 4];
+    }
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+        if (first + 256u * u >= total) continue;
+        // levels, exact, times the scale: exact down to float32's smallest number (a scale of 255: not a number, times zero too)
+        const float scale = byte[u] == 255 ? __uint_as_float(0x7fc00000u) : scale_value(static_cast<uint32_t>(byte[u]));
+        const f32x2 q[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 1),
+                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 3)};
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = q[e >> 1][e & 1] * scale;
+        store_eight<TYPE>(out + p[u].row * ld + p[u].at * 8, x, static_cast<int>(d - p[u].at * 8));
     }
 }
 
@@ -137,16 +178,19 @@ static int32_t check_matrix(const void *v, int32_t type, int64_t cols, int64_t l
     if (!v || !typed(type) || ld < cols || reinterpret_cast<uintptr_t>(v) % wide_of(type)) return DQ_ERR_INVALID_ARG;
     return DQ_OK;
 }
-static unsigned blocks_of(int64_t threads) { return static_cast<unsigned>(std::clamp<int64_t>((threads + 255) / 256, 1, 1 << 20)); }
-// rows of 8 numbers that can be read 16 bytes at a time
-static bool wide_reads(const void *v, int32_t type, int64_t ld) { return aligned16(v) && ld * wide_of(type) % 16 == 0; }
-
+// Blocks for n rows of `per` items; rows: how many a blockIdx.y takes.
+static dim3 blocks_of(int64_t n, int64_t per, int at_once, int64_t &rows)
+{
+    rows = std::min<int64_t>(n, std::max<int64_t>((1ll << 31) / per, (n + 65534) / 65535));
+    return dim3(static_cast<unsigned>((rows * per + 256 * at_once - 1) / (256 * at_once)), static_cast<unsigned>((n + rows - 1) / rows));
+}
 template <int TYPE>
 static int32_t quantize4(const void *v, int64_t ld, const dq_mx4 &q, uint32_t *status, hipStream_t st)
 {
-    mx4_quantize_kernel<TYPE><<<blocks_of(q.n * groups_of(q.d) * 16), 256, 0, st>>>(static_cast<const typename Num<TYPE>::Mem *>(v), q.n, q.d, ld,
-                                                                                    wide_reads(v, TYPE, ld), q.codes, q.ld_codes, q.scales, q.ld_scales,
-                                                                                    status);
+    int64_t rows;
+    const dim3 blocks = blocks_of(q.n, groups_of(q.d) * 16, 1, rows);
+    mx4_quantize_kernel<TYPE><<<blocks, 256, 0, st>>>(static_cast<const typename Num<TYPE>::Mem *>(v), q.n, rows, static_cast<uint32_t>(q.d), ld,
+                                                      q.codes, q.ld_codes, q.scales, q.ld_scales, status);
     DQ_LAUNCH_CHECK();
     return DQ_OK;
 }
@@ -157,6 +201,18 @@ static int32_t quantize4(const void *v, int32_t type, int64_t ld, const dq_mx4 &
     case DQ_F16: return quantize4<DQ_F16>(v, ld, q, status, st);
     default: return quantize4<DQ_BF16>(v, ld, q, status, st);
     }
+}
+
+template <int TYPE>
+static int32_t dequantize4(const dq_mx4 &q, void *out, int64_t ld, hipStream_t st)
+{
+    constexpr int kAtOnce = TYPE == DQ_F32 ? 1 : 4;
+    int64_t rows;
+    const dim3 blocks = blocks_of(q.n, (q.d + 7) / 8, kAtOnce, rows);
+    mx4_dequantize_kernel<TYPE, kAtOnce><<<blocks, 256, 0, st>>>(q.codes, q.ld_codes, q.scales, q.ld_scales, q.n, rows, static_cast<uint32_t>(q.d),
+                                                        static_cast<typename Num<TYPE>::Mem *>(out), ld);
+    DQ_LAUNCH_CHECK();
+    return DQ_OK;
 }
 
 template <int TYPE, int kXT, int YT, int WX, int WY, int H>
@@ -206,15 +262,11 @@ extern "C" int32_t dq_mx4_dequantize(const dq_mx4 *q, void *out, int32_t type, i
     if (const int32_t e = dq::check4(q)) return e;
     if (const int32_t e = dq::check_matrix(out, type, q->d, ld)) return e;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const int vector = dq::four_at_once(out, ld, dq::wide_of(type));
-    const unsigned blocks = dq::blocks_of(q->n * ((q->d + 7) / 8));
     switch (type) {
-    case DQ_F32: dq::mx4_dequantize_kernel<DQ_F32><<<blocks, 256, 0, st>>>(q->codes, q->ld_codes, q->scales, q->ld_scales, q->n, q->d, static_cast<float *>(out), ld, vector); break;
-    case DQ_F16: dq::mx4_dequantize_kernel<DQ_F16><<<blocks, 256, 0, st>>>(q->codes, q->ld_codes, q->scales, q->ld_scales, q->n, q->d, static_cast<dq::u16 *>(out), ld, vector); break;
-    default: dq::mx4_dequantize_kernel<DQ_BF16><<<blocks, 256, 0, st>>>(q->codes, q->ld_codes, q->scales, q->ld_scales, q->n, q->d, static_cast<dq::u16 *>(out), ld, vector); break;
+    case DQ_F32: return dq::dequantize4<DQ_F32>(*q, out, ld, st);
+    case DQ_F16: return dq::dequantize4<DQ_F16>(*q, out, ld, st);
+    default: return dq::dequantize4<DQ_BF16>(*q, out, ld, st);
     }
-    DQ_LAUNCH_CHECK();
-    return DQ_OK;
 }
 
 extern "C" int32_t dq_mx4_product(const dq_mx4 *a, const dq_mx4 *w, void *out, int32_t type, int64_t ld, void *stream)
