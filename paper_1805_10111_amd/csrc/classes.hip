@@ -202,17 +202,17 @@ __global__ __launch_bounds__(kTeacherThreads) void teacher_kernel(const int32_t 
 __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // The sums of a tile's row: its maximum, the sum of exp above it, the targets' sum q z; [tile][row].
-template <int TYPE, int XT, int YT, int WX, int WY, int H>
+template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, float inv_tau, Targets targets,
                                                                int tiles_x, int tiles_y, float2 *__restrict__ sums, float *__restrict__ hits)
 {
-    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H> Tile;
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H, R, P> Tile;
     __shared__ float3 shared[WX][YT];
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t c0 = static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
     Tile tile;
-    tile.template run<TYPE == DQ_F32>(w, a, c0, t0, 0, k);
+    tile.run(w, a, c0, t0, 0, k);
     const int lane = threadIdx.x & 63, wave_c0 = static_cast<int>(c0) + Tile::sub_x(0) * 16;
 #pragma unroll
     for (int y = 0; y < Tile::SY; ++y) {
@@ -325,18 +325,18 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2 *__restrict__ 
 
 // ---- gradients -----------------------------------------------------------------
 // g of a piece of the classes, [rows of the tiles][ldg] in 16 bits (three planes for float32); zeros where there is no row or class.
-template <int TYPE, int XT, int YT, int WX, int WY, int H>
+template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, int64_t piece0,
                                                              int64_t piece, float inv_tau, Targets targets, const float *__restrict__ lse,
                                                              const float *__restrict__ weight, const float *__restrict__ weight_max,
                                                              int tiles_x, int tiles_y, u16 *__restrict__ g, int64_t ldg, int64_t plane)
 {
-    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H> Tile;
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H, R, P> Tile;
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t c0 = piece0 + static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
     Tile tile;
-    tile.template run<TYPE == DQ_F32>(w, a, c0, t0, 0, k);
+    tile.run(w, a, c0, t0, 0, k);
     const int wave_c0 = static_cast<int>(c0) + Tile::sub_x(0) * 16;
 #pragma unroll
     for (int y = 0; y < Tile::SY; ++y) {
@@ -396,20 +396,20 @@ __device__ __forceinline__ float gradient_unit(int type, float post, const float
 
 // da of a piece, one split of its classes per blockIdx.y: partial sums [split][n][ldp] in float32, added to what the pieces before left.
 // Where one launch has it all (partial null) da itself.
-template <int TYPE, int XT, int YT, int WX, int WY, int H>
+template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void da_kernel(Operand w, Operand g, int64_t piece, int64_t per_split, int64_t n, int64_t d, int tiles_x,
                                                            int tiles_y, float *__restrict__ partial, int64_t ldp, int first, Targets targets, float post,
                                                            const float *__restrict__ weight_max, typename Num<TYPE>::Mem *__restrict__ da,
                                                            int64_t ldda, int vector)
 {
-    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, false, H> Tile;
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, false, H, R, P> Tile;
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t i0 = static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT, k0 = blockIdx.y * per_split;
     const int64_t k1 = lesser(k0 + per_split, piece);
     if (k0 >= k1 && !first) return;
     Tile tile;
-    tile.template run<TYPE == DQ_F32>(w, g, i0, t0, k0, k0 < k1 ? k1 : k0);
+    tile.run(w, g, i0, t0, k0, k0 < k1 ? k1 : k0);
     float *const out = partial + blockIdx.y * n * ldp;
     const float unit = gradient_unit(TYPE, post, weight_max);
 #pragma unroll
@@ -450,17 +450,17 @@ __global__ __launch_bounds__(256) void da_finish_kernel(const float *__restrict_
     }
 }
 
-template <int TYPE, int XT, int YT, int WX, int WY, int H>
+template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void dw_kernel(Operand a, Operand g, int64_t k, int64_t piece, int64_t d, int tiles_x, int tiles_y,
                                                            float post, const float *__restrict__ weight_max,
                                                            typename Num<TYPE>::Mem *__restrict__ dw, int64_t lddw)
 {
-    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, true, H> Tile;
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, true, true, H, R, P> Tile;
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t i0 = static_cast<int64_t>(tx) * XT, j0 = static_cast<int64_t>(ty) * YT;
     Tile tile;
-    tile.template run<TYPE == DQ_F32>(a, g, i0, j0, 0, k);
+    tile.run(a, g, i0, j0, 0, k);
     const float unit = gradient_unit(TYPE, post, weight_max);
     tile.store(dw + j0 * lddw + i0, lddw, piece - j0, d - i0, [&](int m, int n) { return quad_of<TYPE>(tile.acc[m][n] * unit); });
 }
@@ -480,8 +480,9 @@ struct ClassPlan {
     int64_t n, c, d, k, dp;             // dp: columns of packed rows
     bool direct_a, direct_w;
     TileSize tile, tile_da, tile_dw;
-    int64_t xt, yt, tiles_x, tiles_y;   // of scores
-    int64_t piece, pieces, ldg, rows_g, rows_z, xd, yd, splits, per_split;
+    TileDims td, td_da, td_dw;
+    int64_t tiles_x, tiles_y;           // of scores
+    int64_t piece, pieces, ldg, rows_g, rows_z, splits, per_split;
     bool da_at_once;
     int64_t cls, q, entropy, weight_max, lse, sums, hits, a, w, az, g, partial, bytes;
 };
@@ -508,11 +509,11 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
     // there meets the zeros behind the features' rows.  (Odd rows would lose the last number at the end of the memory.)
     s.direct_a = s.planes == 1 && s.d % 32 == 0 && p->lda % 8 == 0 && pa % 16 == 0;
     s.direct_w = s.planes == 1 && s.d % 2 == 0 && p->ldw % 8 == 0 && pw % 16 == 0;
-    s.tile = tile_for_rows(s.c, s.n);
-    s.yt = side(s.tile);
-    s.xt = s.tile == kTile16 ? 64 : s.yt;
-    s.tiles_x = (s.c + s.xt - 1) / s.xt;
-    s.tiles_y = (s.n + s.yt - 1) / s.yt;
+    const bool parts = s.planes > 1;
+    s.tile = tile_for_rows(s.c, s.n, parts);
+    s.td = dims_of(s.tile, parts, false);
+    s.tiles_x = (s.c + s.td.x - 1) / s.td.x;
+    s.tiles_y = (s.n + s.td.y - 1) / s.td.y;
     if (s.tiles_x * s.tiles_y > kMost) return DQ_ERR_UNSUPPORTED;
     int64_t at = 0;
     s.cls = room(at, k ? 4 * s.n * s.k : 0);
@@ -526,19 +527,19 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
     s.w = room(at, s.direct_w ? 0 : 2 * s.planes * s.c * s.dp);
     if (grad) {
         s.rows_z = up(s.n, 32);
-        s.rows_g = s.tiles_y * s.yt;
+        s.rows_g = s.tiles_y * s.td.y;
         const int64_t most = std::max<int64_t>(kPieceBytes / (2 * s.planes * s.rows_g) / 256, 1) * 256;
         s.pieces = (s.c + most - 1) / most;
         s.piece = up((s.c + s.pieces - 1) / s.pieces, 256);
         s.pieces = (s.c + s.piece - 1) / s.piece;
         s.ldg = s.piece;
-        s.tile_dw = s.n <= 64 && s.c * s.d <= (1 << 20) ? kTile64 : tile_for(s.d, std::min(s.c, s.piece));
+        s.tile_dw = s.n <= 64 && s.c * s.d <= (1 << 20) ? kTileFew : tile_for(s.d, std::min(s.c, s.piece), parts);
+        s.td_dw = dims_of(s.tile_dw, parts, true);
         // da has few tiles: its classes are split until the chip is full (a block per compute unit, smaller tiles two or more), though not
         // below four steps each.
-        s.tile_da = s.n <= 16 ? kTile16 : s.n <= 64 ? kTile64 : s.n * s.d <= 256 * 1024 ? kTile128 : kTile256;
-        s.yd = side(s.tile_da);
-        s.xd = s.tile_da == kTile16 ? 128 : s.yd;
-        const int64_t tiles = (s.d + s.xd - 1) / s.xd * ((s.n + s.yd - 1) / s.yd), blocks = s.tile_da == kTile256 ? 256 : 512;
+        s.tile_da = s.n <= 16 ? kTileFewest : s.n <= 64 ? kTileFew : s.n * s.d <= 256 * 1024 ? kTileMiddle : kTileLarge;
+        s.td_da = dims_of(s.tile_da, parts, true);
+        const int64_t tiles = tiles_of(s.d, s.n, s.td_da), blocks = s.tile_da == kTileLarge ? 256 : 512;
         const int64_t most_splits = std::clamp<int64_t>(s.piece / 128, 1, std::max<int64_t>(blocks / tiles, 1));
         s.splits = 1;
         double best = 1e30;
@@ -576,19 +577,6 @@ struct ClassCall {
     char *ws;
     hipStream_t st;
 };
-
-// One launch of a kernel template in the tile size that a plan names (wavefronts WX x WY, steps a stage); `few`: what it is launched as
-// for 16 rows.
-#define DQ_TILE_LAUNCH(size, kernel, few, grid, ...)                                                               \
-    do {                                                                                                           \
-        switch (size) {                                                                                            \
-        case kTile256: kernel<TYPE, 256, 256, 2, 4, 1><<<grid, 512, 0, st>>>(__VA_ARGS__); break;                     \
-        case kTile128: kernel<TYPE, 128, 128, 2, 2, 1><<<grid, 256, 0, st>>>(__VA_ARGS__); break;                     \
-        case kTile64: kernel<TYPE, 64, 64, 2, 2, 2><<<grid, 256, 0, st>>>(__VA_ARGS__); break;                        \
-        case kTile16: few<<<grid, 256, 0, st>>>(__VA_ARGS__); break;                                               \
-        }                                                                                                          \
-        DQ_LAUNCH_CHECK();                                                                                         \
-    } while (0)
 
 template <int TYPE>
 static int32_t class_run(const ClassCall &q, const ClassPlan &s)
@@ -635,7 +623,12 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     float2 *const sums = reinterpret_cast<float2 *>(ws + s.sums);
     float *const hits = reinterpret_cast<float *>(ws + s.hits), *const lse = reinterpret_cast<float *>(ws + s.lse);
     const int tiles_x = static_cast<int>(s.tiles_x), tiles_y = static_cast<int>(s.tiles_y);
-    DQ_TILE_LAUNCH(s.tile, scores_kernel, (scores_kernel<TYPE, 64, 16, 4, 1, 2>), static_cast<unsigned>(tiles_x * tiles_y), w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits);
+#define DQ_GRID(threads) grid, threads, 0, st
+    constexpr bool kInParts = TYPE == DQ_F32;
+    constexpr int kH = kInParts ? 1 : 2, kP = kInParts ? 3 : 1;
+    dim3 grid(static_cast<unsigned>(tiles_x * tiles_y));
+    DQ_TILE_CASE(scores_kernel, TYPE, kInParts, s.tile, (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits)
+    DQ_LAUNCH_CHECK();
     if (n <= 256) finish_kernel<1><<<static_cast<unsigned>(n), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
     else finish_kernel<16><<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
     DQ_LAUNCH_CHECK();
@@ -656,21 +649,28 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     Mem *const da = static_cast<Mem *>(q.da);
     for (int64_t at = 0; at < c; at += s.piece) {
         const int64_t have = std::min(s.piece, c - at);
-        const int tiles_p = static_cast<int>((have + s.xt - 1) / s.xt);
-        DQ_TILE_LAUNCH(s.tile, grad_kernel, (grad_kernel<TYPE, 64, 16, 4, 1, 2>), static_cast<unsigned>(tiles_p * tiles_y), w, a, kd, n, c, at, have, 1.0f / tau, targets, lse, q.weight, weight_max,
-                       tiles_p, tiles_y, g, s.ldg, plane);
+        const int tiles_p = static_cast<int>((have + s.td.x - 1) / s.td.x);
+        grid = dim3(static_cast<unsigned>(tiles_p * tiles_y));
+        DQ_TILE_CASE(grad_kernel, TYPE, kInParts, s.tile, (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
+                     q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
+        DQ_LAUNCH_CHECK();
         if (q.da) {
             const Operand piece{w.p + at * w.ld, w.ld, c - at, w.cols, w.plane};
-            const int tx = static_cast<int>((s.d + s.xd - 1) / s.xd), ty = static_cast<int>((n + s.yd - 1) / s.yd);
-            DQ_TILE_LAUNCH(s.tile_da, da_kernel, (da_kernel<TYPE, 128, 16, 4, 1, 2>), dim3(static_cast<unsigned>(tx * ty), static_cast<unsigned>(s.splits)), piece, go, up(have, 32), s.per_split, n,
-                           s.d, tx, ty, partial, s.dp, at == 0, targets, post, weight_max, da, q.ldda, vector_da);
+            const int tx = static_cast<int>((s.d + s.td_da.x - 1) / s.td_da.x), ty = static_cast<int>((n + s.td_da.y - 1) / s.td_da.y);
+            grid = dim3(static_cast<unsigned>(tx * ty), static_cast<unsigned>(s.splits));
+            DQ_TILE_CASE(da_kernel, TYPE, kInParts, s.tile_da, (da_kernel<TYPE, 128, 16, 4, 1, kH, 4, kP>), DQ_GRID, piece, go, up(have, 32), s.per_split, n, s.d, tx,
+                         ty, partial, s.dp, at == 0, targets, post, weight_max, da, q.ldda, vector_da)
+            DQ_LAUNCH_CHECK();
         }
         if (q.dw) {
-            const int t = side(s.tile_dw), tx = static_cast<int>((s.d + t - 1) / t), ty = static_cast<int>((have + t - 1) / t);
-            DQ_TILE_LAUNCH(s.tile_dw, dw_kernel, (dw_kernel<TYPE, 64, 64, 2, 2, 2>), static_cast<unsigned>(tx * ty), az, go, s.rows_z, have, s.d, tx, ty, post, weight_max,
-                           static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw);
+            const int tx = static_cast<int>((s.d + s.td_dw.x - 1) / s.td_dw.x), ty = static_cast<int>((have + s.td_dw.y - 1) / s.td_dw.y);
+            grid = dim3(static_cast<unsigned>(tx * ty));
+            DQ_TILE_CASE(dw_kernel, TYPE, kInParts, s.tile_dw, (dw_kernel<TYPE, 64, 64, 2, 2, kH, 4, kP>), DQ_GRID, az, go, s.rows_z, have, s.d, tx, ty, post, weight_max,
+                         static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw)
+            DQ_LAUNCH_CHECK();
         }
     }
+#undef DQ_GRID
     if (q.da && partial) {
         const int64_t blocks = std::min<int64_t>((n * ((s.d + 3) / 4) + 255) / 256, 1 << 16);
         da_finish_kernel<TYPE><<<static_cast<unsigned>(blocks), 256, 0, st>>>(partial, static_cast<int>(s.splits), n, s.d, s.dp, targets, post, weight_max, da,

@@ -47,10 +47,10 @@ struct Operand {
 };
 
 // float32 numbers are carried as three bfloat16 (24 bits of significand between them): x y = the products of the parts whose
-// exponents add up to at least that of the last bit, six of nine, smallest first.  Two bits per step: which part of x, of y.
-constexpr int kPartSteps = 6;
-constexpr uint32_t kPartsX = 2u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 0u << 10;
-constexpr uint32_t kPartsY = 0u | 2u << 2 | 1u << 4 | 0u << 6 | 1u << 8 | 0u << 10;
+// exponents add up to at least that of the last bit, six of nine, smallest first: which part of x, of y.  All parts of a stage lie in
+// LDS together, so that each is brought there once for the products it has a share in.
+constexpr int kPartProducts = 6;
+constexpr int kPartsX[kPartProducts] = {2, 0, 1, 1, 0, 0}, kPartsY[kPartProducts] = {0, 2, 1, 0, 1, 0};
 
 struct MulBf16 {
     static constexpr bool kScaled = false;
@@ -113,11 +113,13 @@ struct StageLoads {
     static constexpr int kPairMask = T / 16 >= 8 ? 7 : T / 16 - 1;
     uint32_t off[kChunks];
 
-    // loads of any thread in the first of `slices` slices
-    static constexpr int first(int slices)
+    // The loads of `planes` parts of numbers are asked for in slices; how many of any thread are in the first.
+    static constexpr int slice_of(int plane, int i, int planes, int slices) { return (plane * kChunks + i) * slices / (planes * kChunks); }
+    static constexpr int first(int planes, int slices)
     {
         int n = 0;
-        for (int i = 0; i < kSurely; ++i) n += i * slices / kChunks == 0;
+        for (int p = 0; p < planes; ++p)
+            for (int i = 0; i < kSurely; ++i) n += slice_of(p, i, planes, slices) == 0;
         return n;
     }
 
@@ -132,13 +134,13 @@ struct StageLoads {
             off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(o.ld) + static_cast<uint32_t>(at);
         }
     }
-    // `part` of `parts` of the loads; to: where this wavefront's first one goes.  wide: bytes of k there are yet; a stage of several
+    // Those of a plane that are in this slice; to: where this wavefront's first one goes.  wide: bytes of k there are yet; a stage of several
     // steps may end behind them, and what lies there, in the next row, is not read but zeros are.
-    __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t from, char *ring, int to, int part, int parts, int wide) const
+    __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t from, char *ring, int to, int plane, int planes, int slice, int slices, int wide) const
     {
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
-            if (i * parts / kChunks != part) continue;
+            if (slice_of(plane, i, planes, slices) != slice) continue;
             if (kChunks != kSurely && static_cast<int>(threadIdx.x) + i * THREADS >= kAll) continue;      // (whole wavefronts)
             uint32_t at = off[i];
             if constexpr (H > 1 && !ACROSS) {
@@ -178,11 +180,11 @@ struct Reader {
         edge = same(edge);
     }
     static __device__ __forceinline__ int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
-    // any: whether there is another stage
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(bool any) const
+    // any: whether there is another stage.  plane: bytes further on.
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(bool any, int64_t plane) const
     {
         const int32_t bytes = max(ACROSS ? min(left, kStepRows * H) * ld + edge : left, 0);
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p), 0, any ? bytes : 0, 0x00027000);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p + plane), 0, any ? bytes : 0, 0x00027000);
     }
     __device__ __forceinline__ void next()
     {
@@ -220,7 +222,8 @@ __device__ __forceinline__ i32x4 stage_part(const char *ring, int from, int addr
 }
 
 // WX x WY wavefronts share the tile.  Each of them multiplies SX x SY subtiles.
-template <class Mul, int XT, int YT, int WX, int WY, bool XS, bool YS, int H = 1>
+// H steps a stage, R stages in the ring (an even number), P parts of a number.
+template <class Mul, int XT, int YT, int WX, int WY, bool XS, bool YS, int H, int R, int P>
 struct TileProduct {
     static constexpr int kThreads = WX * WY * kWave;
     static constexpr int SX = XT / 16 / WX, SY = YT / 16 / WY;
@@ -282,28 +285,38 @@ struct TileProduct {
 
     // A stage is multiplied in parts: H steps, kQ of x's subtiles at a time; what a part multiplies has been read from LDS a part before.
     static constexpr int kQ = SX < 4 ? SX : 4, kPer = SX / kQ, kParts = H * kPer;
-    static constexpr int kY = XT * kStepBytes * H;           // where y's part of a stage begins
-    __device__ __forceinline__ void read_part(const char *ring, int part, i32x4 (&x)[kQ], i32x4 (&y)[SY]) const
+    static constexpr int kPlaneX = XT * kStepBytes * H, kPlaneY = YT * kStepBytes * H, kY = P * kPlaneX;      // where y's part of a stage begins
+    __device__ __forceinline__ void read_part(const char *ring, int part, i32x4 (&x)[P][kQ], i32x4 (&y)[P][SY]) const
     {
         const int half = part / kPer, q = part % kPer;
         if (q == 0)
 #pragma unroll
-            for (int n = 0; n < SY; ++n) y[n] = stage_part<YT, YS, H>(ring, kY, address_y, half, n);
+            for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int m = 0; m < kQ; ++m) x[m] = stage_part<XT, XS, H>(ring, 0, address_x, half, q * kQ + m);
+                for (int n = 0; n < SY; ++n) y[p][n] = stage_part<YT, YS, H>(ring, kY + p * kPlaneY, address_y, half, n);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int m = 0; m < kQ; ++m) x[p][m] = stage_part<XT, XS, H>(ring, p * kPlaneX, address_x, half, q * kQ + m);
     }
-    __device__ __forceinline__ void multiply_part(const i32x4 (&x)[kQ], const i32x4 (&y)[SY], int part, const Scales &scales)
+    __device__ __forceinline__ void multiply_part(const i32x4 (&x)[P][kQ], const i32x4 (&y)[P][SY], int part, const Scales &scales)
     {
         const int half = part / kPer, q = part % kPer;
 #pragma unroll
-        for (int m = 0; m < kQ; ++m)
+        for (int i = 0; i < (P > 1 ? kPartProducts : 1); ++i)
 #pragma unroll
-            for (int n = 0; n < SY; ++n) {
-                const int at = q * kQ + m;
-                f32x4 &c = acc[at][n];
-                if constexpr (Mul::kScaled) c = Mul::mul(x[m], y[n], c, static_cast<int>(scales.x[half][at / 4]), at % 4, static_cast<int>(scales.y[half][n / 4]), n % 4);
-                else c = Mul::mul(x[m], y[n], c);
-            }
+            for (int m = 0; m < kQ; ++m)
+#pragma unroll
+                for (int n = 0; n < SY; ++n) {
+                    const int at = q * kQ + m;
+                    f32x4 &c = acc[at][n];
+                    if constexpr (Mul::kScaled)
+                        c = Mul::mul(x[0][m], y[0][n], c, static_cast<int>(scales.x[half][at / 4]), at % 4, static_cast<int>(scales.y[half][n / 4]), n % 4);
+                    else if constexpr (P > 1)
+                        c = Mul::mul(x[kPartsX[i]][m], y[kPartsY[i]][n], c);
+                    else
+                        c = Mul::mul(x[0][m], y[0][n], c);
+                }
     }
     // In what order a part's instructions are issued: the next part's reads of LDS between the first products, so that each has the
     // rest of the part to arrive (left to itself the compiler puts them right before their use).
@@ -319,7 +332,7 @@ struct TileProduct {
         __builtin_amdgcn_sched_group_barrier(kMatrix, PRODUCTS, 0);
     }
 
-    static constexpr int kRingBytes = (XT + YT) * kStepBytes * H;
+    static constexpr int kRingBytes = P * (XT + YT) * kStepBytes * H;
     // the first stage's memory; the results pass through it
     static __device__ __forceinline__ char *first_ring()
     {
@@ -374,12 +387,12 @@ struct TileProduct {
             }
     }
 
-    // k0 .. k1 (in pairs of bytes, multiples of 32) of rows i0.. of x and j0.. of y.  PARTS: operands are float32 in parts.
-    template <bool PARTS>
+    // k0 .. k1 (in pairs of bytes, multiples of 32) of rows i0.. of x and j0.. of y.
     __device__ __forceinline__ void run(const Operand &x, const Operand &y, int64_t i0, int64_t j0, int64_t k0, int64_t k1)
     {
         // (an array of its own for each stage: the compiler keeps apart what is read and what is arriving by the array, up to seven)
-        __shared__ __attribute__((aligned(1024))) char ring1[kRingBytes], ring2[kRingBytes], ring3[kRingBytes];
+        static_assert((R == 2 || R == 4) && (!Mul::kScaled || R == 4), "rings of two and four are written out below");
+        __shared__ __attribute__((aligned(1024))) char ring1[kRingBytes], ring2[R > 2 ? kRingBytes : 16], ring3[R > 2 ? kRingBytes : 16];
         char *const ring0 = first_ring();
         __shared__ __attribute__((aligned(16))) uint8_t scales0[Mul::kScaled ? kScaleBytes * H : 16], scales1[Mul::kScaled ? kScaleBytes * H : 16];
         typedef StageLoads<XT, XS, kThreads, H> LoadsX;
@@ -392,44 +405,31 @@ struct TileProduct {
         for (int m = 0; m < SX; ++m)
 #pragma unroll
             for (int n = 0; n < SY; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int per = static_cast<int>((k1 - k0 + 32 * H - 1) / (32 * H)), stages = PARTS ? per * kPartSteps : per;
+        const int stages = static_cast<int>((k1 - k0 + 32 * H - 1) / (32 * H));
         if (stages <= 0) return;
         address_x = part_address<XT, XS, H>(sub_x(0));
         address_y = part_address<YT, YS, H>(sub_y(0));
-        const Reader<XT, XS, H> bx(x, i0, k0);
-        const Reader<YT, YS, H> by(y, j0, k0);
-        Reader<XT, XS, H> rx = bx;
-        Reader<YT, YS, H> ry = by;
-        int coming = stages, at = per, part = 0;     // stages to be loaded yet, of this product of parts
-        auto select = [&] {
-            rx = bx;
-            ry = by;
-            rx.p += ((kPartsX >> (2 * part)) & 3) * x.plane;
-            ry.p += ((kPartsY >> (2 * part)) & 3) * y.plane;
-        };
-        if constexpr (PARTS) select();
-        // Loads of a stage, asked for in kSlices slices.  Behind the last stage they find nothing and bring zeros, so that every wavefront
-        // has as many loads under way as ever.
-        constexpr int kSlices = kParts > 1 ? 2 : 1;
+        Reader<XT, XS, H> rx(x, i0, k0);
+        Reader<YT, YS, H> ry(y, j0, k0);
+        int coming = stages, wide = static_cast<int>(k1 - k0) * 2;      // stages to be loaded yet, bytes of k they hold
+        // Loads of a stage, asked for in kSlices slices: right behind the barrier that frees its place in the ring, and a part later.
+        // Behind the last stage they find nothing and bring zeros, so that every wavefront has as many loads under way as ever.
+        constexpr int kSlices = kParts > 1 && R > 2 ? 2 : 1;
         const int to = wave() * kWave * 16;
         auto load = [&](char *ring, int slice) {
-            const int wide = static_cast<int>(k1 - k0) * 2 - (per - at) * kStepBytes * H;
-            lx.issue(rx.buffer(coming > 0), ring, to, slice, kSlices, wide);
-            ly.issue(ry.buffer(coming > 0), ring, kY + to, slice, kSlices, wide);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                lx.issue(rx.buffer(coming > 0, p * x.plane), ring, p * kPlaneX + to, p, P, slice, kSlices, wide);
+                ly.issue(ry.buffer(coming > 0, p * y.plane), ring, kY + p * kPlaneY + to, p, P, slice, kSlices, wide);
+            }
             if (slice + 1 < kSlices) return;
             --coming;
+            wide -= kStepBytes * H;
             rx.next();
             ry.next();
-            if (PARTS || H > 1) --at;
-            if constexpr (PARTS)
-                if (at == 0) {
-                    at = per;
-                    ++part;
-                    select();
-                }
         };
         static_assert(H == 1 || H * kPer % 2 == 0, "parity");
-        i32x4 px[2][kQ], py[2][SY];             // of a part and of the next: x by the part, y by the step
+        i32x4 px[2][P][kQ], py[2][P][SY];       // of a part and of the next: x by the part, y by the step
         Scales scales{}, scales_next{};
         Brought brought[2] = {}, scales_at[2] = {};      // scales on their way to LDS, by the stage; of the first two stages
         const uint8_t *row = nullptr;
@@ -447,21 +447,23 @@ struct TileProduct {
             for (int slice = 0; slice < kSlices; ++slice) load(ring, slice);
         };
         load_all(ring0);
-        load_all(ring1);
-        load_all(ring2);
-        if (kSlices > 1) load(ring3, 0);
+        if constexpr (R > 2) {
+            load_all(ring1);
+            load_all(ring2);
+        }
+        load(R > 2 ? ring3 : ring1, 0);
         if constexpr (Mul::kScaled) {
             write_scales(scales0, scales_at[0]);
             write_scales(scales1, scales_at[1]);
         }
         // loads that every wavefront has under way per stage, of a first slice
-        constexpr int kEach = LoadsX::kSurely + LoadsY::kSurely, kFirst = kSlices > 1 ? LoadsX::first(kSlices) + LoadsY::first(kSlices) : 0;
-        stage_arrived<2 * kEach + kFirst>();
+        constexpr int kEach = P * (LoadsX::kSurely + LoadsY::kSurely), kFirst = LoadsX::first(P, kSlices) + LoadsY::first(P, kSlices);
+        stage_arrived<(R - 2) * kEach + kFirst>();
         read_part(ring0, 0, px[0], py[0]);
         if constexpr (Mul::kScaled) read_scales(scales0, scales);
         // Stage s out of `now`; `next` holds the next one, the second slice of `later` is still to be asked for.
         auto stage = [&](char *now, char *next, char *later, uint8_t *ss, uint8_t *sn, int parity, int s) {
-            constexpr int kPerX = XS ? 2 : 1, kPerY = YS ? 2 : 1;
+            constexpr int kPerX = P * (XS ? 2 : 1), kPerY = P * (YS ? 2 : 1), kProducts = (P > 1 ? kPartProducts : 1) * kQ * SY;
 #pragma unroll
             for (int part = 0; part < kParts; ++part) {
                 __builtin_amdgcn_sched_barrier(0);
@@ -469,31 +471,37 @@ struct TileProduct {
                 const int y_next = (part + 1) % kPer ? yours : yours ^ 1;
                 if (part + 1 < kParts) {
                     read_part(now, part + 1, px[mine ^ 1], py[y_next]);
-                    if (part == 0) load(later, 1);
+                    if (part == 0 && kSlices > 1) load(later, 1);
                 } else {
-                    stage_arrived<(kSlices > 1 ? 2 : 1) * kEach>();      // the next stage's; what was asked for since then is on its way
+                    stage_arrived<(R - 2) * kEach>();                    // the next stage's; what was asked for since then is on its way
                     if constexpr (Mul::kScaled) {
                         read_scales(sn, scales_next);                    // written before this barrier
                         write_scales(ss, brought[parity]);               // stage s + 2's; what was there was read before it
                         brought[parity] = load_scales(row, s + 4, groups);
                     }
                     read_part(next, 0, px[mine ^ 1], py[y_next]);        // (after the last stage: zeros)
-                    load(kSlices > 1 ? now : later, 0);
+                    load(now, 0);
                 }
                 multiply_part(px[mine], py[yours], part, scales);
-                if ((part + 1) % kPer) order_part<kQ * kPerX, kQ * SY>();
-                else order_part<kQ * kPerX + SY * kPerY, kQ * SY>();
+                if ((part + 1) % kPer) order_part<kQ * kPerX, kProducts>();
+                else order_part<kQ * kPerX + SY * kPerY, kProducts>();
             }
             if constexpr (Mul::kScaled) scales = scales_next;
         };
-        for (int s = 0; s < stages; s += kRing) {
-            stage(ring0, ring1, ring3, scales0, scales1, 0, s);
-            if (s + 1 >= stages) break;
-            stage(ring1, ring2, ring0, scales1, scales0, 1, s + 1);
-            if (s + 2 >= stages) break;
-            stage(ring2, ring3, ring1, scales0, scales1, 0, s + 2);
-            if (s + 3 >= stages) break;
-            stage(ring3, ring0, ring2, scales1, scales0, 1, s + 3);
+        for (int s = 0; s < stages; s += R) {
+            if constexpr (R == 2) {
+                stage(ring0, ring1, ring1, scales0, scales1, 0, s);
+                if (s + 1 >= stages) break;
+                stage(ring1, ring0, ring0, scales1, scales0, 1, s + 1);
+            } else {
+                stage(ring0, ring1, ring3, scales0, scales1, 0, s);
+                if (s + 1 >= stages) break;
+                stage(ring1, ring2, ring0, scales1, scales0, 1, s + 1);
+                if (s + 2 >= stages) break;
+                stage(ring2, ring3, ring1, scales0, scales1, 0, s + 2);
+                if (s + 3 >= stages) break;
+                stage(ring3, ring0, ring2, scales1, scales0, 1, s + 3);
+            }
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);     // nothing is on its way to LDS any more
     }
@@ -572,20 +580,38 @@ __device__ __forceinline__ void tile_of_block(int block, int tiles_x, int tiles_
 // Tiles of the products.  What a tile's side costs in the efficiency of the matrix cores it gains where there are few tiles: measured on
 // large products 256 x 256 reaches 1170 to 1330 TFLOP/s, 128 x 128 820 to 1120; 8192 rows of the smaller one's blocks, two to a compute
 // unit, take 1.4 times as long as the larger's for the same work.
-enum TileSize { kTile256, kTile128, kTile64, kTile16 };      // the last: 16 rows by 64 (classes) or 128 (columns)
-
-constexpr int side(TileSize s) { return s == kTile256 ? 256 : s == kTile128 ? 128 : s == kTile64 ? 64 : 16; }
-
-// The larger tile, unless the rounds its blocks take on 256 compute units are so much emptier than the smaller's that those are faster.
-inline TileSize tile_for(int64_t x, int64_t y)
+enum TileSize { kTileLarge, kTileMiddle, kTileFew, kTileFewest };
+struct TileDims {
+    int x, y;
+};
+// x by y results a tile.  float32 in parts takes three times the room in LDS, and tiles half as high.  The last: 64 by 16 rows, of 128
+// columns where x is stored across k.
+constexpr TileDims dims_of(TileSize s, bool parts, bool across)
 {
-    const int64_t big = (x + 255) / 256 * ((y + 255) / 256), small = (x + 127) / 128 * ((y + 127) / 128);
-    return 1.4 * 0.5 * static_cast<double>((small + 511) / 512) < static_cast<double>((big + 255) / 256) ? kTile128 : kTile256;
+    return s == kTileLarge ? TileDims{256, parts ? 128 : 256} : s == kTileMiddle ? TileDims{128, parts ? 64 : 128} : s == kTileFew ? TileDims{64, 64} : TileDims{across ? 128 : 64, 16};
+}
+inline int64_t tiles_of(int64_t x, int64_t y, TileDims t) { return (x + t.x - 1) / t.x * ((y + t.y - 1) / t.y); }
+
+// The larger tile, unless the rounds its blocks take on 256 compute units are so much emptier than the smaller's, two to a compute unit, that
+// those are faster.
+inline TileSize tile_for(int64_t x, int64_t y, bool parts)
+{
+    const int64_t large = tiles_of(x, y, dims_of(kTileLarge, parts, false)), middle = tiles_of(x, y, dims_of(kTileMiddle, parts, false));
+    return 1.4 * 0.5 * static_cast<double>((middle + 511) / 512) < static_cast<double>((large + 255) / 256) ? kTileMiddle : kTileLarge;
 }
 // ... of products over `rows` rows.
-inline TileSize tile_for_rows(int64_t x, int64_t rows)
+inline TileSize tile_for_rows(int64_t x, int64_t rows, bool parts)
 {
-    return rows <= 16 ? kTile16 : rows <= 64 ? kTile64 : tile_for(x, rows);
+    return rows <= 16 ? kTileFewest : rows <= 64 ? kTileFew : tile_for(x, rows, parts);
 }
+
+// kernel<what, x, y, WX, WY, H, R, P> in a tile's size: its wavefronts, steps a stage, stages in the ring, parts of a number.
+#define DQ_TILE_CASE(kernel, what, parts, size, few, launch, ...)                                                              \
+    switch (size) {                                                                                                            \
+    case kTileLarge: kernel<what, 256, parts ? 128 : 256, 2, 4, 1, parts ? 2 : 4, parts ? 3 : 1><<<launch(512)>>>(__VA_ARGS__); break;     \
+    case kTileMiddle: kernel<what, 128, parts ? 64 : 128, 2, 2, 1, parts ? 2 : 4, parts ? 3 : 1><<<launch(256)>>>(__VA_ARGS__); break;     \
+    case kTileFew: kernel<what, 64, 64, 2, 2, parts ? 1 : 2, 4, parts ? 3 : 1><<<launch(256)>>>(__VA_ARGS__); break;          \
+    case kTileFewest: few<<<launch(256)>>>(__VA_ARGS__); break;                                                                \
+    }
 
 }  // namespace dq

@@ -147,16 +147,16 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__re
     }
 }
 
-template <int TYPE, int XT, int YT, int WX, int WY, int H>
+template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void mx4_product_kernel(Operand w, Operand a, int64_t k, int tiles_x, int tiles_y,
                                                                     typename Num<TYPE>::Mem *__restrict__ out, int64_t ld)
 {
-    typedef TileProduct<MulMx4, XT, YT, WX, WY, false, false, H> Tile;
+    typedef TileProduct<MulMx4, XT, YT, WX, WY, false, false, H, R, P> Tile;
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t i0 = static_cast<int64_t>(tx) * XT, j0 = static_cast<int64_t>(ty) * YT;
     Tile tile;
-    tile.template run<false>(w, a, i0, j0, 0, k);
+    tile.run(w, a, i0, j0, 0, k);
     tile.store(out + j0 * ld + i0, ld, a.rows - j0, w.rows - i0, [&](int m, int n) { return quad_of<TYPE>(tile.acc[m][n]); });
 }
 
@@ -215,26 +215,20 @@ static int32_t dequantize4(const dq_mx4 &q, void *out, int64_t ld, hipStream_t s
     return DQ_OK;
 }
 
-template <int TYPE, int kXT, int YT, int WX, int WY, int H>
-static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int64_t ld, hipStream_t st)
-{
-    const int64_t tiles_x = (w.n + kXT - 1) / kXT, tiles_y = (a.n + YT - 1) / YT;
-    if (tiles_x * tiles_y > kMost4) return DQ_ERR_UNSUPPORTED;
-    auto operand = [](const dq_mx4 &q) { return Operand{reinterpret_cast<const char *>(q.codes), q.ld_codes, q.n, static_cast<int32_t>(groups_of(q.d) * 32), 0, q.scales, q.ld_scales}; };
-    mx4_product_kernel<TYPE, kXT, YT, WX, WY, H><<<static_cast<unsigned>(tiles_x * tiles_y), WX * WY * kWave, 0, st>>>(
-        operand(w), operand(a), groups_of(a.d) * 32, static_cast<int>(tiles_x), static_cast<int>(tiles_y), static_cast<typename Num<TYPE>::Mem *>(out), ld);
-    DQ_LAUNCH_CHECK();
-    return DQ_OK;
-}
 template <int TYPE>
 static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int64_t ld, hipStream_t st)
 {
-    switch (tile_for_rows(w.n, a.n)) {
-    case kTile256: return product4<TYPE, 256, 256, 2, 4, 1>(a, w, out, ld, st);
-    case kTile128: return product4<TYPE, 128, 128, 2, 2, 1>(a, w, out, ld, st);
-    case kTile64: return product4<TYPE, 64, 64, 2, 2, 2>(a, w, out, ld, st);
-    default: return product4<TYPE, 64, 16, 4, 1, 2>(a, w, out, ld, st);
-    }
+    const TileSize size = tile_for_rows(w.n, a.n, false);
+    const TileDims t = dims_of(size, false, false);
+    const int64_t tiles_x = (w.n + t.x - 1) / t.x, tiles_y = (a.n + t.y - 1) / t.y;
+    if (tiles_x * tiles_y > kMost4) return DQ_ERR_UNSUPPORTED;
+    auto operand = [](const dq_mx4 &q) { return Operand{reinterpret_cast<const char *>(q.codes), q.ld_codes, q.n, static_cast<int32_t>(groups_of(q.d) * 32), 0, q.scales, q.ld_scales}; };
+#define DQ_GRID(threads) static_cast<unsigned>(tiles_x * tiles_y), threads, 0, st
+    DQ_TILE_CASE(mx4_product_kernel, TYPE, false, size, (mx4_product_kernel<TYPE, 64, 16, 4, 1, 2, 4, 1>), DQ_GRID, operand(w), operand(a), groups_of(a.d) * 32,
+                 static_cast<int>(tiles_x), static_cast<int>(tiles_y), static_cast<typename Num<TYPE>::Mem *>(out), ld)
+#undef DQ_GRID
+    DQ_LAUNCH_CHECK();
+    return DQ_OK;
 }
 static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int32_t type, int64_t ld, hipStream_t st)
 {
