@@ -324,7 +324,7 @@ int32_t dq_acc_snapshot(const float *xsum, int64_t m, int64_t d, float *x_snap_o
 #define DQ_BF16  2
 
 /* Host struct: n rows of features and a model of c classes, both d wide; lda, ldw: elements from one row to the next (>= d; any,
- * as any alignment to the element, but rows that are 16-byte aligned with d % 32 == 0 are read in place). */
+ * as any alignment to the element, but 16-bit rows that are 16-byte aligned with d % 8 == 0 are read in place). */
 typedef struct dq_classes {
     int32_t type;                    /* DQ_F32, DQ_F16, DQ_BF16 */
     int64_t n, c, d;

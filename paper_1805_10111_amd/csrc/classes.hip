@@ -118,17 +118,19 @@ __global__ __launch_bounds__(256) void pack_kernel(Packed a, Packed w, int64_t o
     }
 }
 
-// The largest |weight| of a call in float16, one block.
-__global__ __launch_bounds__(1024) void weight_max_kernel(const float *__restrict__ weight, int64_t n, float *__restrict__ out)
+// The largest |weight| of the rows that have a target, for float16, one block.  Held between 2^-100 and the largest finite number: an
+// infinite weight is its own row's matter.
+__global__ __launch_bounds__(1024) void weight_max_kernel(const float *__restrict__ weight, int64_t n, Targets targets, float *__restrict__ out)
 {
     __shared__ uint32_t top;
     if (threadIdx.x == 0) top = 0;
     __syncthreads();
     uint32_t m = 0;
-    for (int64_t t = threadIdx.x; t < n; t += 1024) m = max(m, __float_as_uint(weight[t]) & 0x7fffffffu);
+    for (int64_t t = threadIdx.x; t < n; t += 1024)
+        if (targets.used(t)) m = max(m, __float_as_uint(weight[t]) & 0x7fffffffu);
     atomicMax(&top, m);
     __syncthreads();
-    if (threadIdx.x == 0) out[0] = top ? __uint_as_float(top) : 1.0f;
+    if (threadIdx.x == 0) out[0] = top ? __uint_as_float(min(max(top, 0x0d800000u), 0x7f7fffffu)) : 1.0f;
 }
 
 // One block of 64 threads per row: q = softmax(logit / tau) over the entries, sorted by class (bitonic, in LDS).
@@ -201,12 +203,15 @@ __global__ __launch_bounds__(kTeacherThreads) void teacher_kernel(const int32_t 
 // ---- scores --------------------------------------------------------------------
 __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
+constexpr int kEdge = 4;               // with a type: rows that are read in place end inside of a step
+
 // The sums of a tile's row: its maximum, the sum of exp above it, the targets' sum q z; [tile][row].
-template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
+template <int WHAT, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, float inv_tau, Targets targets,
                                                                int tiles_x, int tiles_y, float2 *__restrict__ sums, float *__restrict__ hits)
 {
-    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H, R, P> Tile;
+    constexpr int TYPE = WHAT & 3;
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H, R, P, (WHAT & kEdge) != 0> Tile;
     __shared__ float3 shared[WX][YT];
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
@@ -325,13 +330,14 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2 *__restrict__ 
 
 // ---- gradients -----------------------------------------------------------------
 // g of a piece of the classes, [rows of the tiles][ldg] in 16 bits (three planes for float32); zeros where there is no row or class.
-template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
+template <int WHAT, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, int64_t piece0,
                                                              int64_t piece, float inv_tau, Targets targets, const float *__restrict__ lse,
                                                              const float *__restrict__ weight, const float *__restrict__ weight_max,
                                                              int tiles_x, int tiles_y, u16 *__restrict__ g, int64_t ldg, int64_t plane)
 {
-    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H, R, P> Tile;
+    constexpr int TYPE = WHAT & 3;
+    typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H, R, P, (WHAT & kEdge) != 0> Tile;
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t c0 = piece0 + static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
@@ -505,10 +511,9 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
     s.d = p->d;
     s.k = k ? k : 1;
     s.dp = up(s.d, 64);
-    // The model is read in place where its rows are whole 16-byte chunks, also if they end inside of a step of 32 columns: what follows
-    // there meets the zeros behind the features' rows.  (Odd rows would lose the last number at the end of the memory.)
-    s.direct_a = s.planes == 1 && s.d % 32 == 0 && p->lda % 8 == 0 && pa % 16 == 0;
-    s.direct_w = s.planes == 1 && s.d % 2 == 0 && p->ldw % 8 == 0 && pw % 16 == 0;
+    // Read in place where rows are whole 16-byte chunks, also if they end inside of a step of 32 columns.
+    s.direct_a = s.planes == 1 && s.d % 8 == 0 && p->lda % 8 == 0 && pa % 16 == 0;
+    s.direct_w = s.planes == 1 && s.d % 8 == 0 && p->ldw % 8 == 0 && pw % 16 == 0;
     const bool parts = s.planes > 1;
     s.tile = tile_for_rows(s.c, s.n, parts);
     s.td = dims_of(s.tile, parts, false);
@@ -627,7 +632,10 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     constexpr bool kInParts = TYPE == DQ_F32;
     constexpr int kH = kInParts ? 1 : 2, kP = kInParts ? 3 : 1;
     dim3 grid(static_cast<unsigned>(tiles_x * tiles_y));
-    DQ_TILE_CASE(scores_kernel, TYPE, kInParts, s.tile, (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits)
+    constexpr int kEdged = kInParts ? TYPE : TYPE | kEdge;
+    const bool edge = (s.direct_a || s.direct_w) && s.d % 32;
+    if (edge) DQ_TILE_CASE(scores_kernel, kEdged, kInParts, s.tile, (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits)
+    else DQ_TILE_CASE(scores_kernel, TYPE, kInParts, s.tile, (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits)
     DQ_LAUNCH_CHECK();
     if (n <= 256) finish_kernel<1><<<static_cast<unsigned>(n), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
     else finish_kernel<16><<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
@@ -638,7 +646,7 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     float *weight_max = nullptr;
     if (TYPE == DQ_F16 && q.weight) {
         weight_max = reinterpret_cast<float *>(ws + s.weight_max);
-        weight_max_kernel<<<1, 1024, 0, st>>>(q.weight, n, weight_max);
+        weight_max_kernel<<<1, 1024, 0, st>>>(q.weight, n, targets, weight_max);
         DQ_LAUNCH_CHECK();
     }
     u16 *const g = reinterpret_cast<u16 *>(ws + s.g);
@@ -651,8 +659,10 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
         const int64_t have = std::min(s.piece, c - at);
         const int tiles_p = static_cast<int>((have + s.td.x - 1) / s.td.x);
         grid = dim3(static_cast<unsigned>(tiles_p * tiles_y));
-        DQ_TILE_CASE(grad_kernel, TYPE, kInParts, s.tile, (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
-                     q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
+        if (edge) DQ_TILE_CASE(grad_kernel, kEdged, kInParts, s.tile, (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
+                               q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
+        else DQ_TILE_CASE(grad_kernel, TYPE, kInParts, s.tile, (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
+                          q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
         DQ_LAUNCH_CHECK();
         if (q.da) {
             const Operand piece{w.p + at * w.ld, w.ld, c - at, w.cols, w.plane};

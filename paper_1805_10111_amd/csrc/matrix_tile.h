@@ -35,12 +35,12 @@ constexpr int kStepRows = 32;                  // of k, for an operand stored ac
 constexpr int kRing = 4;                       // stages in LDS, of H steps each
 
 // An operand in memory.  Its row i (row k where it is stored across k) begins at p + i * ld bytes; rows is how many there are.
-// Nothing outside of it is read: rows past the last are zeros, and k past its end.
+// Nothing outside of it matters: rows past the last are zeros, and k past its end.
 struct Operand {
     const char *p;
     int64_t ld;            // bytes, a multiple of 16
     int64_t rows;
-    int32_t cols;          // numbers of a row (pairs of bytes); even.  Along k: numbers of k behind them are zeros only in the last row
+    int32_t cols;          // numbers of a row (pairs of bytes), a multiple of 8.  Along k those behind them are zeros, whatever lies there
     int64_t plane;         // bytes from one part of a number to the next (float32 as three bfloat16), 0 otherwise
     const uint8_t *scales; // 4-bit numbers: four scales per 64 bytes of a row, from row to row ld_scales bytes
     int64_t ld_scales;
@@ -104,7 +104,8 @@ __device__ __forceinline__ void stage_arrived()
 // LDS holds a stage as it lies in memory, its 16-byte chunks permuted within a row so that no two of the lanes that read together
 // meet a bank: along k, chunk c of row r at c ^ (r H / 4) % 4H (16 lanes read 16 rows of 64 H bytes); across k, 32 bytes at a time,
 // pair c of row k at c ^ (k % 4 + 4 (k / 8 % 2)) (32 lanes read rows k .. k + 3 and k + 8 .. k + 11).
-template <int T, bool ACROSS, int THREADS, int H>
+// EDGE: rows may end inside of a step (which costs a comparison a load: 2% of a large product).
+template <int T, bool ACROSS, int THREADS, int H, bool EDGE>
 struct StageLoads {
     static constexpr int kAll = T * 4 * H;                                       // 16-byte chunks of a stage
     static constexpr int kChunks = (kAll + THREADS - 1) / THREADS;               // loads of a thread per stage
@@ -134,8 +135,8 @@ struct StageLoads {
             off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(o.ld) + static_cast<uint32_t>(at);
         }
     }
-    // Those of a plane that are in this slice; to: where this wavefront's first one goes.  wide: bytes of k there are yet; a stage of several
-    // steps may end behind them, and what lies there, in the next row, is not read but zeros are.
+    // Those of a plane that are in this slice; to: where this wavefront's first one goes.  wide: bytes of k there are yet; a stage may end
+    // behind them, and what lies there (the next row, or what a wider matrix holds between the rows) is not read but zeros are.
     __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t from, char *ring, int to, int plane, int planes, int slice, int slices, int wide) const
     {
 #pragma unroll
@@ -143,7 +144,7 @@ struct StageLoads {
             if (slice_of(plane, i, planes, slices) != slice) continue;
             if (kChunks != kSurely && static_cast<int>(threadIdx.x) + i * THREADS >= kAll) continue;      // (whole wavefronts)
             uint32_t at = off[i];
-            if constexpr (H > 1 && !ACROSS) {
+            if constexpr (!ACROSS && (H > 1 || EDGE)) {
                 const int id = threadIdx.x + i * THREADS, row = id / kRowChunks;
                 if (((id % kRowChunks) ^ ((row * H / 4) & (4 * H - 1))) * 16 >= wide) at = 0x7fffffff;      // behind every buffer
             }
@@ -223,7 +224,7 @@ __device__ __forceinline__ i32x4 stage_part(const char *ring, int from, int addr
 
 // WX x WY wavefronts share the tile.  Each of them multiplies SX x SY subtiles.
 // H steps a stage, R stages in the ring (an even number), P parts of a number.
-template <class Mul, int XT, int YT, int WX, int WY, bool XS, bool YS, int H, int R, int P>
+template <class Mul, int XT, int YT, int WX, int WY, bool XS, bool YS, int H, int R, int P, bool EDGE = false>
 struct TileProduct {
     static constexpr int kThreads = WX * WY * kWave;
     static constexpr int SX = XT / 16 / WX, SY = YT / 16 / WY;
@@ -395,8 +396,8 @@ struct TileProduct {
         __shared__ __attribute__((aligned(1024))) char ring1[kRingBytes], ring2[R > 2 ? kRingBytes : 16], ring3[R > 2 ? kRingBytes : 16];
         char *const ring0 = first_ring();
         __shared__ __attribute__((aligned(16))) uint8_t scales0[Mul::kScaled ? kScaleBytes * H : 16], scales1[Mul::kScaled ? kScaleBytes * H : 16];
-        typedef StageLoads<XT, XS, kThreads, H> LoadsX;
-        typedef StageLoads<YT, YS, kThreads, H> LoadsY;
+        typedef StageLoads<XT, XS, kThreads, H, EDGE> LoadsX;
+        typedef StageLoads<YT, YS, kThreads, H, EDGE> LoadsY;
         LoadsX lx;
         LoadsY ly;
         lx.init(x);
@@ -411,7 +412,8 @@ struct TileProduct {
         address_y = part_address<YT, YS, H>(sub_y(0));
         Reader<XT, XS, H> rx(x, i0, k0);
         Reader<YT, YS, H> ry(y, j0, k0);
-        int coming = stages, wide = static_cast<int>(k1 - k0) * 2;      // stages to be loaded yet, bytes of k they hold
+        // stages to be loaded yet, bytes of k that they hold of a row (4-bit rows end with a group of 128 numbers, one step)
+        int coming = stages, wide_x = static_cast<int>(XS ? 0 : lesser(k1, x.cols) - k0) * 2, wide_y = static_cast<int>(YS ? 0 : lesser(k1, y.cols) - k0) * 2;
         // Loads of a stage, asked for in kSlices slices: right behind the barrier that frees its place in the ring, and a part later.
         // Behind the last stage they find nothing and bring zeros, so that every wavefront has as many loads under way as ever.
         constexpr int kSlices = kParts > 1 && R > 2 ? 2 : 1;
@@ -419,12 +421,13 @@ struct TileProduct {
         auto load = [&](char *ring, int slice) {
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                lx.issue(rx.buffer(coming > 0, p * x.plane), ring, p * kPlaneX + to, p, P, slice, kSlices, wide);
-                ly.issue(ry.buffer(coming > 0, p * y.plane), ring, kY + p * kPlaneY + to, p, P, slice, kSlices, wide);
+                lx.issue(rx.buffer(coming > 0, p * x.plane), ring, p * kPlaneX + to, p, P, slice, kSlices, wide_x);
+                ly.issue(ry.buffer(coming > 0, p * y.plane), ring, kY + p * kPlaneY + to, p, P, slice, kSlices, wide_y);
             }
             if (slice + 1 < kSlices) return;
             --coming;
-            wide -= kStepBytes * H;
+            wide_x -= kStepBytes * H;
+            wide_y -= kStepBytes * H;
             rx.next();
             ry.next();
         };

@@ -351,3 +351,37 @@ def test_in_a_graph(dq):
         torch.cuda.synchronize()
         for k in out:
             assert torch.equal(out[k], eager[k]), (step, k)
+
+
+@pytest.mark.parametrize("n,c,d", [(1, 300, 8), (20, 500, 40), (130, 300, 72), (300, 1031, 200), (520, 4000, 104)])
+@pytest.mark.parametrize("t", list(TYPES))
+def test_what_lies_between_aligned_rows_reaches_nothing(dq, t, n, c, d):
+    """Rows that start on 16 bytes and end inside of a step of 32 columns, in wider matrices of NaNs: read in place, or packed."""
+    a, w, g = make(n, c, d, t, d)
+    label = torch.randint(-1, c, (n,), generator=g, dtype=torch.int32)
+    q = torch.zeros(n, c, dtype=torch.float64)
+    used = label >= 0
+    q[torch.arange(n)[used], label[used].long()] = 1.0
+    want = definition(a, w, q, 1.0, None, 1.0, used)
+    got = run(dq, strided(a.cuda(), 8, 8), strided(w.cuda(), 16, 8), label.cuda(), None, 1.0, lead=8)
+    for k in want:
+        check(got[k], want[k], k)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), 1e30])
+def test_weights_of_rows_left_out_reach_nothing(dq, t, what):
+    n, c, d = 90, 300, 64
+    a, w, g = make(n, c, d, t, 21)
+    label = torch.randint(0, c, (n,), generator=g, dtype=torch.int32)
+    label[::3] = -1
+    weight = 0.5 + torch.rand(n, generator=g)
+    clean = run(dq, a.cuda(), w.cuda(), label.cuda(), weight.cuda(), 1.0)
+    weight[::3] = what
+    got = run(dq, a.cuda(), w.cuda(), label.cuda(), weight.cuda(), 1.0)
+    for k in clean:
+        # (in float16 the products are held as multiples of the largest weight: the rows that are left out do not count)
+        if t == "f16" and k in ("da", "dw"):
+            assert torch.isfinite(got[k]).all() and (got[k] - clean[k]).abs().max() <= 2 * half_step(TYPES[t]) * clean[k].abs().max(), k
+        else:
+            assert torch.equal(got[k], clean[k]), k
