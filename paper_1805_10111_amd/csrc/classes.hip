@@ -4,9 +4,10 @@
 // The scores z = a W^T / tau are made tile by tile and never stored:
 //   teacher   a teacher's entries in order of class, with their weights q
 //   pack      operands that the matrix cores cannot read in place
-//   scores    one tile of z: per row its maximum, the sum of exp above it and the targets' sum q z
+//   scores    one tile of z: per row its maximum, the sum of exp above it and the targets' sum q z; for gradients the first piece's z too
 //   finish    lse and loss of a row from its tiles
-//   grad      (a piece of the classes at a time) the tile again, now g = f (exp(z - lse) - q), rounded to 16 bits
+//   kept      g = f (exp(z - lse) - q) of the first piece from its z, rounded to 16 bits, where they lie
+//   grad      (the other pieces) the tile again, now g
 //   da        += g W of the piece, split over its classes where there are few tiles
 //   dw        = g^T a of the piece
 #include <algorithm>
@@ -205,10 +206,34 @@ __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp
 
 constexpr int kEdge = 4;               // with a type: rows that are read in place end inside of a step
 
+// The scores of the first piece stay in the place of its gradients, 16 bits of them in each plane: as they are, in two halves, in float32
+// and where there are few rows; else how far they lie below the tile's maximum, in steps of 2^-9 of a factor of two (2^-11 in float16)
+// up to a factor of 2^-128 (2^-32), behind which probabilities are zeros.  That is off by half a step, a factor of 1 -+ 0.0007
+// (0.00017): a fifth (a third) of what g's own rounding may be.  The targets' scores, where p - q may cancel, are kept whole.
+struct Kept {
+    u16 *g;                            // null: none
+    int64_t ldg, plane, cols;          // numbers; classes of the piece
+    float *target_z;                   // z of the targets' entries, null in calls without gradients
+};
+constexpr bool kept_whole(int type, int x) { return type == DQ_F32 || x <= 64; }
+template <int TYPE>
+struct KeptUnit {
+    static constexpr float kSteps = TYPE == DQ_F16 ? 2048.0f : 512.0f;
+    static __device__ __forceinline__ u16 code(float top, float z)
+    {
+        return static_cast<u16>(static_cast<uint32_t>(fminf((top - z) * (1.44269504f * kSteps) + 0.5f, 65535.0f)));
+    }
+    // shift: log2 of exp(top - lse); a row whose lse is not a number has no number
+    static __device__ __forceinline__ float value(u16 code, float shift)
+    {
+        return code == 65535 && shift == shift ? 0.0f : __builtin_amdgcn_exp2f(shift - static_cast<float>(code) * (1.0f / kSteps));
+    }
+};
+
 // The sums of a tile's row: its maximum, the sum of exp above it, the targets' sum q z; [tile][row].
 template <int WHAT, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, float inv_tau, Targets targets,
-                                                               int tiles_x, int tiles_y, float2 *__restrict__ sums, float *__restrict__ hits)
+                                                               int tiles_x, int tiles_y, float2 *__restrict__ sums, float *__restrict__ hits, Kept kept)
 {
     constexpr int TYPE = WHAT & 3;
     typedef TileProduct<typename Num<TYPE>::Mul, XT, YT, WX, WY, false, false, H, R, P, (WHAT & kEdge) != 0> Tile;
@@ -256,6 +281,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operan
 #pragma unroll
                     for (int i = 0; i < 4; ++i) z = rel == 16 * m + i ? tile.acc[m][y][i] : z;
                 hit += q == 0.0f ? 0.0f : q * z;
+                if (kept.target_z && rel >= 0 && rel < Tile::SX * 16 && (rel & 15) < 4) kept.target_z[t * targets.k + e] = z;
             }
         }
         hit += __shfl_xor(hit, 16);
@@ -276,6 +302,32 @@ __global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operan
         }
         sums[static_cast<int64_t>(tx) * n + t0 + r] = make_float2(top, sum);
         hits[static_cast<int64_t>(tx) * n + t0 + r] = hit;
+    }
+    if (!kept.g || c0 >= kept.cols) return;
+    u16 *const to = kept.g + t0 * kept.ldg + c0;
+    if constexpr (kept_whole(TYPE, XT)) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            tile.store(to + p * kept.plane, kept.ldg, YT, XT, [&](int m, int y) {
+                u16x4 r;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r[i] = static_cast<u16>(__float_as_uint(tile.acc[m][y][i]) >> (16 * p));
+                return r;
+            });
+    } else {
+        float top[Tile::SY];
+#pragma unroll
+        for (int y = 0; y < Tile::SY; ++y) {
+            top[y] = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < WX; ++x) top[y] = fmaxf(top[y], shared[x][Tile::at_y(y)].x);
+        }
+        tile.store(to, kept.ldg, YT, XT, [&](int m, int y) {
+            u16x4 r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = KeptUnit<TYPE>::code(top[y], tile.acc[m][y][i]);
+            return r;
+        });
     }
 }
 
@@ -329,7 +381,83 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2 *__restrict__ 
 }
 
 // ---- gradients -----------------------------------------------------------------
-// g of a piece of the classes, [rows of the tiles][ldg] in 16 bits (three planes for float32); zeros where there is no row or class.
+// What a row's gradients are multiplied by in g.
+template <int TYPE>
+__device__ __forceinline__ float row_factor(const float *weight, const float *weight_max, int64_t t, bool live)
+{
+    const float f = live && weight ? weight[t] : 1.0f;
+    return TYPE == DQ_F16 ? f * (kF16Unit / (weight ? weight_max[0] : 1.0f)) : f;
+}
+
+// g of the first piece from what was kept of its scores, in its place: columns 0 .. cols of `rows` rows.  A block takes 2048 columns of
+// a row, eight a thread, and then the targets among them.  What bounds it is memory: it reads and writes g once.
+template <int TYPE, int XT>
+__global__ __launch_bounds__(256) void kept_kernel(Kept kept, int64_t cols, int64_t rows, int64_t n, const float2 *__restrict__ sums, Targets targets,
+                                                   const float *__restrict__ lse, const float *__restrict__ weight,
+                                                   const float *__restrict__ weight_max)
+{
+    typedef __attribute__((ext_vector_type(8))) u16 Eight;
+    constexpr bool kWhole = kept_whole(TYPE, XT);
+    constexpr int kPlanes = TYPE == DQ_F32 ? 3 : 1;
+    const int64_t first = blockIdx.x * 2048ll, i = first + threadIdx.x * 8;
+    for (int64_t t = blockIdx.y; t < rows; t += gridDim.y) {
+        const bool live = t < n && targets.used(t);
+        u16 *const row = kept.g + t * kept.ldg;
+        const float from = live ? lse[t] : 0.0f, f = row_factor<TYPE>(weight, weight_max, t, live);
+        if (i < cols) {
+            Eight out[kPlanes] = {};
+            if (live) {
+                const Eight lo = *reinterpret_cast<const Eight *>(row + i);
+                float p[8];
+                if constexpr (kWhole) {
+                    const Eight hi = *reinterpret_cast<const Eight *>(row + kept.plane + i);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float z = __uint_as_float(static_cast<uint32_t>(hi[e]) << 16 | lo[e]) - from;
+                        p[e] = TYPE == DQ_F32 ? expf(z) : exp_near(z);
+                    }
+                } else {
+                    const float shift = (sums[i / XT * n + t].x - from) * 1.44269504f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[e] = KeptUnit<TYPE>::value(lo[e], shift);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (TYPE == DQ_F32) {
+                        u16 part[3];
+                        parts_of(f * p[e], part);
+#pragma unroll
+                        for (int h = 0; h < 3; ++h) out[h][e] = part[h];
+                    } else {
+                        out[0][e] = Num<TYPE>::store(f * p[e]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < kPlanes; ++h) *reinterpret_cast<Eight *>(row + h * kept.plane + i) = out[h];
+        }
+        __syncthreads();
+        if (!live) continue;
+        const int32_t *const cls = targets.cls + t * targets.k;
+        const int end = static_cast<int>(lesser(first + 2048, kept.cols));
+        for (int e = targets.first(t, static_cast<int>(first)) + threadIdx.x; e < targets.k && cls[e] < end; e += 256) {
+            if (e && cls[e - 1] == cls[e]) continue;           // (the first of a class that comes several times takes them all)
+            const float z = kept.target_z[t * targets.k + e] - from;
+            float v = TYPE == DQ_F32 ? expf(z) : exp_near(z);
+            for (int o = e; o < targets.k && cls[o] == cls[e]; ++o) v -= targets.q ? targets.q[t * targets.k + o] : 1.0f;
+            if constexpr (TYPE == DQ_F32) {
+                u16 part[3];
+                parts_of(f * v, part);
+#pragma unroll
+                for (int h = 0; h < 3; ++h) row[h * kept.plane + cls[e]] = part[h];
+            } else {
+                row[cls[e]] = Num<TYPE>::store(f * v);
+            }
+        }
+    }
+}
+
+// g of another piece of the classes, [rows of the tiles][ldg] in 16 bits (three planes for float32); zeros where there is no row or class.
 template <int WHAT, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, int64_t piece0,
                                                              int64_t piece, float inv_tau, Targets targets, const float *__restrict__ lse,
@@ -350,8 +478,7 @@ __global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand 
         const bool live = t < n && targets.used(t);
         const int base = static_cast<int>(c0) + Tile::at_x(0);
         const float from = live ? lse[t] : 0.0f;
-        float f = live && weight ? weight[t] : 1.0f;
-        if constexpr (TYPE == DQ_F16) f = f * (kF16Unit / (weight ? weight_max[0] : 1.0f));
+        const float f = row_factor<TYPE>(weight, weight_max, t, live);
 #pragma unroll
         for (int m = 0; m < Tile::SX; ++m)
 #pragma unroll
@@ -488,9 +615,9 @@ struct ClassPlan {
     TileSize tile, tile_da, tile_dw;
     TileDims td, td_da, td_dw;
     int64_t tiles_x, tiles_y;           // of scores
-    int64_t piece, pieces, ldg, rows_g, rows_z, splits, per_split;
+    int64_t piece, pieces, ldg, rows_g, rows_z, planes_g, splits, per_split;
     bool da_at_once;
-    int64_t cls, q, entropy, weight_max, lse, sums, hits, a, w, az, g, partial, bytes;
+    int64_t cls, q, entropy, weight_max, lse, target_z, sums, hits, a, w, az, g, partial, bytes;
 };
 
 static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &s)
@@ -533,9 +660,10 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
     if (grad) {
         s.rows_z = up(s.n, 32);
         s.rows_g = s.tiles_y * s.td.y;
-        const int64_t most = std::max<int64_t>(kPieceBytes / (2 * s.planes * s.rows_g) / 256, 1) * 256;
+        s.planes_g = std::max(s.planes, kept_whole(s.type, s.td.x) ? 2 : 1);
+        const int64_t most = std::max<int64_t>(kPieceBytes / (2 * s.planes_g * s.rows_g) / 256, 1) * 256;
         s.pieces = (s.c + most - 1) / most;
-        s.piece = up((s.c + s.pieces - 1) / s.pieces, 256);
+        s.piece = s.pieces > 1 ? most : up(s.c, 256);          // (the first one's scores are kept: it takes all that there is room for)
         s.pieces = (s.c + s.piece - 1) / s.piece;
         s.ldg = s.piece;
         s.tile_dw = s.n <= 64 && s.c * s.d <= (1 << 20) ? kTileFew : tile_for(s.d, std::min(s.c, s.piece), parts);
@@ -559,7 +687,8 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
         s.splits = (s.piece + s.per_split - 1) / s.per_split;
         s.da_at_once = s.splits == 1 && s.pieces == 1;
         s.az = room(at, 2 * s.planes * s.rows_z * s.dp);
-        s.g = room(at, 2 * s.planes * s.rows_g * s.ldg);
+        s.target_z = room(at, 4 * s.n * s.k);
+        s.g = room(at, 2 * s.planes_g * s.rows_g * s.ldg);
         s.partial = room(at, s.da_at_once ? 0 : 4 * s.splits * s.n * s.dp);
     }
     s.bytes = up(at, 16);
@@ -632,15 +761,20 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     constexpr bool kInParts = TYPE == DQ_F32;
     constexpr int kH = kInParts ? 1 : 2, kP = kInParts ? 3 : 1;
     dim3 grid(static_cast<unsigned>(tiles_x * tiles_y));
+    // gradients: kept of the first piece
+    const bool products = q.grad && (q.da || q.dw);
+    const int64_t plane = s.rows_g * s.ldg;
+    u16 *const g = reinterpret_cast<u16 *>(ws + s.g);
+    const Kept kept = products ? Kept{g, s.ldg, plane, std::min(s.piece, c), reinterpret_cast<float *>(ws + s.target_z)} : Kept{};
     constexpr int kEdged = kInParts ? TYPE : TYPE | kEdge;
     const bool edge = (s.direct_a || s.direct_w) && s.d % 32;
-    if (edge) DQ_TILE_CASE(scores_kernel, kEdged, kInParts, s.tile, (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits)
-    else DQ_TILE_CASE(scores_kernel, TYPE, kInParts, s.tile, (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits)
+    if (edge) DQ_TILE_CASE(scores_kernel, kEdged, kInParts, s.tile, (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept)
+    else DQ_TILE_CASE(scores_kernel, TYPE, kInParts, s.tile, (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept)
     DQ_LAUNCH_CHECK();
     if (n <= 256) finish_kernel<1><<<static_cast<unsigned>(n), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
     else finish_kernel<16><<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
     DQ_LAUNCH_CHECK();
-    if (!q.grad || !(q.da || q.dw)) return DQ_OK;
+    if (!products) return DQ_OK;
 
     const float post = q.scale * tau;
     float *weight_max = nullptr;
@@ -649,20 +783,29 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
         weight_max_kernel<<<1, 1024, 0, st>>>(q.weight, n, targets, weight_max);
         DQ_LAUNCH_CHECK();
     }
-    u16 *const g = reinterpret_cast<u16 *>(ws + s.g);
     float *const partial = s.da_at_once ? nullptr : reinterpret_cast<float *>(ws + s.partial);
-    const int64_t plane = s.rows_g * s.ldg;
-    const Operand go{reinterpret_cast<const char *>(g), s.ldg * 2, s.rows_g, static_cast<int32_t>(s.ldg), plane * 2};
+    const int64_t rows_k = std::min(s.rows_g, s.rows_z);           // of g: nothing else of it is read
+    const Operand go{reinterpret_cast<const char *>(g), s.ldg * 2, rows_k, static_cast<int32_t>(s.ldg), plane * 2};
     const int vector_da = four_at_once(q.da, q.ldda, static_cast<int>(wide));
     Mem *const da = static_cast<Mem *>(q.da);
     for (int64_t at = 0; at < c; at += s.piece) {
         const int64_t have = std::min(s.piece, c - at);
-        const int tiles_p = static_cast<int>((have + s.td.x - 1) / s.td.x);
-        grid = dim3(static_cast<unsigned>(tiles_p * tiles_y));
-        if (edge) DQ_TILE_CASE(grad_kernel, kEdged, kInParts, s.tile, (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
-                               q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
-        else DQ_TILE_CASE(grad_kernel, TYPE, kInParts, s.tile, (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
-                          q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
+        if (at == 0) {
+            const int64_t cols = up(have, 32);
+            const dim3 spans(static_cast<unsigned>((cols + 2047) / 2048), static_cast<unsigned>(std::min<int64_t>(rows_k, 65535)));
+            switch (kInParts ? 64 : s.td.x) {
+            case 64: kept_kernel<TYPE, 64><<<spans, 256, 0, st>>>(kept, cols, rows_k, n, sums, targets, lse, q.weight, weight_max); break;
+            case 128: kept_kernel<TYPE, 128><<<spans, 256, 0, st>>>(kept, cols, rows_k, n, sums, targets, lse, q.weight, weight_max); break;
+            default: kept_kernel<TYPE, 256><<<spans, 256, 0, st>>>(kept, cols, rows_k, n, sums, targets, lse, q.weight, weight_max); break;
+            }
+        } else {
+            const int tiles_p = static_cast<int>((have + s.td.x - 1) / s.td.x);
+            grid = dim3(static_cast<unsigned>(tiles_p * tiles_y));
+            if (edge) DQ_TILE_CASE(grad_kernel, kEdged, kInParts, s.tile, (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
+                                   q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
+            else DQ_TILE_CASE(grad_kernel, TYPE, kInParts, s.tile, (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
+                              q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
+        }
         DQ_LAUNCH_CHECK();
         if (q.da) {
             const Operand piece{w.p + at * w.ld, w.ld, c - at, w.cols, w.plane};
