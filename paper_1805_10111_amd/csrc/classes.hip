@@ -18,7 +18,7 @@
 namespace dq {
 
 constexpr int kNoClass = 0x7fffffff;
-constexpr int64_t kPieceBytes = 512ll << 20;   // of g
+constexpr int64_t kPieceBytes = 1024ll << 20;   // of g
 constexpr float kF16Unit = 16384.0f;           // g of float16: terms down to 2^-29 of the largest weight stay normal
 
 // The three bfloat16 whose sum is v.  Infinities and NaNs: the first part alone.
