@@ -232,7 +232,7 @@ struct KeptUnit {
 
 // The sums of a tile's row: its maximum, the sum of exp above it, the targets' sum q z; [tile][row].
 template <int WHAT, int XT, int YT, int WX, int WY, int H, int R, int P>
-__global__ __launch_bounds__(WX *WY *kWave) void scores_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, float inv_tau, Targets targets,
+__global__ __launch_bounds__(WX *WY *kWave, 2) void scores_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, float inv_tau, Targets targets,
                                                                int tiles_x, int tiles_y, float2 *__restrict__ sums, float *__restrict__ hits, Kept kept)
 {
     constexpr int TYPE = WHAT & 3;
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(256) void kept_kernel(Kept kept, int64_t cols, int6
 
 // g of another piece of the classes, [rows of the tiles][ldg] in 16 bits (three planes for float32); zeros where there is no row or class.
 template <int WHAT, int XT, int YT, int WX, int WY, int H, int R, int P>
-__global__ __launch_bounds__(WX *WY *kWave) void grad_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, int64_t piece0,
+__global__ __launch_bounds__(WX *WY *kWave, 2) void grad_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, int64_t piece0,
                                                              int64_t piece, float inv_tau, Targets targets, const float *__restrict__ lse,
                                                              const float *__restrict__ weight, const float *__restrict__ weight_max,
                                                              int tiles_x, int tiles_y, u16 *__restrict__ g, int64_t ldg, int64_t plane)
@@ -530,7 +530,7 @@ __device__ __forceinline__ float gradient_unit(int type, float post, const float
 // da of a piece, one split of its classes per blockIdx.y: partial sums [split][n][ldp] in float32, added to what the pieces before left.
 // Where one launch has it all (partial null) da itself.
 template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
-__global__ __launch_bounds__(WX *WY *kWave) void da_kernel(Operand w, Operand g, int64_t piece, int64_t per_split, int64_t n, int64_t d, int tiles_x,
+__global__ __launch_bounds__(WX *WY *kWave, 2) void da_kernel(Operand w, Operand g, int64_t piece, int64_t per_split, int64_t n, int64_t d, int tiles_x,
                                                            int tiles_y, float *__restrict__ partial, int64_t ldp, int first, Targets targets, float post,
                                                            const float *__restrict__ weight_max, typename Num<TYPE>::Mem *__restrict__ da,
                                                            int64_t ldda, int vector)
@@ -584,7 +584,7 @@ __global__ __launch_bounds__(256) void da_finish_kernel(const float *__restrict_
 }
 
 template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
-__global__ __launch_bounds__(WX *WY *kWave) void dw_kernel(Operand a, Operand g, int64_t k, int64_t piece, int64_t d, int tiles_x, int tiles_y,
+__global__ __launch_bounds__(WX *WY *kWave, 2) void dw_kernel(Operand a, Operand g, int64_t k, int64_t piece, int64_t d, int tiles_x, int tiles_y,
                                                            float post, const float *__restrict__ weight_max,
                                                            typename Num<TYPE>::Mem *__restrict__ dw, int64_t lddw)
 {
@@ -642,7 +642,7 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
     s.direct_a = s.planes == 1 && s.d % 8 == 0 && p->lda % 8 == 0 && pa % 16 == 0;
     s.direct_w = s.planes == 1 && s.d % 8 == 0 && p->ldw % 8 == 0 && pw % 16 == 0;
     const bool parts = s.planes > 1;
-    s.tile = tile_for_rows(s.c, s.n, parts);
+    s.tile = tile_for_rows(s.c, s.n, parts, true);
     s.td = dims_of(s.tile, parts, false);
     s.tiles_x = (s.c + s.td.x - 1) / s.td.x;
     s.tiles_y = (s.n + s.td.y - 1) / s.td.y;
@@ -666,7 +666,7 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
         s.piece = s.pieces > 1 ? most : up(s.c, 256);          // (the first one's scores are kept: it takes all that there is room for)
         s.pieces = (s.c + s.piece - 1) / s.piece;
         s.ldg = s.piece;
-        s.tile_dw = s.n <= 64 && s.c * s.d <= (1 << 20) ? kTileFew : tile_for(s.d, std::min(s.c, s.piece), parts);
+        s.tile_dw = s.n <= 64 && s.c * s.d <= (1 << 20) ? kTileFew : tile_for(s.d, std::min(s.c, s.piece), parts, true, true);
         s.td_dw = dims_of(s.tile_dw, parts, true);
         // da has few tiles: its classes are split until the chip is full (a block per compute unit, smaller tiles two or more), though not
         // below four steps each.
@@ -757,6 +757,8 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     float2 *const sums = reinterpret_cast<float2 *>(ws + s.sums);
     float *const hits = reinterpret_cast<float *>(ws + s.hits), *const lse = reinterpret_cast<float *>(ws + s.lse);
     const int tiles_x = static_cast<int>(s.tiles_x), tiles_y = static_cast<int>(s.tiles_y);
+// (float32 has no half tiles: the kernel of its middle ones stands there)
+#define DQ_HALF(kernel, what) kernel<what, kInParts ? 128 : 256, kInParts ? 64 : 128, 2, 2, 1, kInParts ? 2 : 3, kP>
 #define DQ_GRID(threads) grid, threads, 0, st
     constexpr bool kInParts = TYPE == DQ_F32;
     constexpr int kH = kInParts ? 1 : 2, kP = kInParts ? 3 : 1;
@@ -768,8 +770,8 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     const Kept kept = products ? Kept{g, s.ldg, plane, std::min(s.piece, c), reinterpret_cast<float *>(ws + s.target_z)} : Kept{};
     constexpr int kEdged = kInParts ? TYPE : TYPE | kEdge;
     const bool edge = (s.direct_a || s.direct_w) && s.d % 32;
-    if (edge) DQ_TILE_CASE(scores_kernel, kEdged, kInParts, s.tile, (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept)
-    else DQ_TILE_CASE(scores_kernel, TYPE, kInParts, s.tile, (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept)
+    if (edge) DQ_TILE_CASE(scores_kernel, kEdged, kInParts, s.tile, (DQ_HALF(scores_kernel, kEdged)), (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept)
+    else DQ_TILE_CASE(scores_kernel, TYPE, kInParts, s.tile, (DQ_HALF(scores_kernel, TYPE)), (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept)
     DQ_LAUNCH_CHECK();
     if (n <= 256) finish_kernel<1><<<static_cast<unsigned>(n), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
     else finish_kernel<16><<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
@@ -801,9 +803,9 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
         } else {
             const int tiles_p = static_cast<int>((have + s.td.x - 1) / s.td.x);
             grid = dim3(static_cast<unsigned>(tiles_p * tiles_y));
-            if (edge) DQ_TILE_CASE(grad_kernel, kEdged, kInParts, s.tile, (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
+            if (edge) DQ_TILE_CASE(grad_kernel, kEdged, kInParts, s.tile, (DQ_HALF(grad_kernel, kEdged)), (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
                                    q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
-            else DQ_TILE_CASE(grad_kernel, TYPE, kInParts, s.tile, (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
+            else DQ_TILE_CASE(grad_kernel, TYPE, kInParts, s.tile, (DQ_HALF(grad_kernel, TYPE)), (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
                               q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
         }
         DQ_LAUNCH_CHECK();
@@ -811,19 +813,20 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
             const Operand piece{w.p + at * w.ld, w.ld, c - at, w.cols, w.plane};
             const int tx = static_cast<int>((s.d + s.td_da.x - 1) / s.td_da.x), ty = static_cast<int>((n + s.td_da.y - 1) / s.td_da.y);
             grid = dim3(static_cast<unsigned>(tx * ty), static_cast<unsigned>(s.splits));
-            DQ_TILE_CASE(da_kernel, TYPE, kInParts, s.tile_da, (da_kernel<TYPE, 128, 16, 4, 1, kH, 4, kP>), DQ_GRID, piece, go, up(have, 32), s.per_split, n, s.d, tx,
+            DQ_TILE_CASE(da_kernel, TYPE, kInParts, s.tile_da, (DQ_HALF(da_kernel, TYPE)), (da_kernel<TYPE, 128, 16, 4, 1, kH, 4, kP>), DQ_GRID, piece, go, up(have, 32), s.per_split, n, s.d, tx,
                          ty, partial, s.dp, at == 0, targets, post, weight_max, da, q.ldda, vector_da)
             DQ_LAUNCH_CHECK();
         }
         if (q.dw) {
             const int tx = static_cast<int>((s.d + s.td_dw.x - 1) / s.td_dw.x), ty = static_cast<int>((have + s.td_dw.y - 1) / s.td_dw.y);
             grid = dim3(static_cast<unsigned>(tx * ty));
-            DQ_TILE_CASE(dw_kernel, TYPE, kInParts, s.tile_dw, (dw_kernel<TYPE, 64, 64, 2, 2, kH, 4, kP>), DQ_GRID, az, go, s.rows_z, have, s.d, tx, ty, post, weight_max,
+            DQ_TILE_CASE(dw_kernel, TYPE, kInParts, s.tile_dw, (DQ_HALF(dw_kernel, TYPE)), (dw_kernel<TYPE, 64, 64, 2, 2, kH, 4, kP>), DQ_GRID, az, go, s.rows_z, have, s.d, tx, ty, post, weight_max,
                          static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw)
             DQ_LAUNCH_CHECK();
         }
     }
 #undef DQ_GRID
+#undef DQ_HALF
     if (q.da && partial) {
         const int64_t blocks = std::min<int64_t>((n * ((s.d + 3) / 4) + 255) / 256, 1 << 16);
         da_finish_kernel<TYPE><<<static_cast<unsigned>(blocks), 256, 0, st>>>(partial, static_cast<int>(s.splits), n, s.d, s.dp, targets, post, weight_max, da,

@@ -402,8 +402,8 @@ struct TileProduct {
     __device__ __forceinline__ void run(const Operand &x, const Operand &y, int64_t i0, int64_t j0, int64_t k0, int64_t k1)
     {
         // (an array of its own for each stage: the compiler keeps apart what is read and what is arriving by the array, up to seven)
-        static_assert((R == 2 || R == 4) && (!Mul::kScaled || R == 4), "rings of two and four are written out below");
-        __shared__ __attribute__((aligned(1024))) char ring1[kRingBytes], ring2[R > 2 ? kRingBytes : 16], ring3[R > 2 ? kRingBytes : 16];
+        static_assert(R >= 2 && R <= 4, "arrays for up to four stages");
+        __shared__ __attribute__((aligned(1024))) char ring1[kRingBytes], ring2[R > 2 ? kRingBytes : 16], ring3[R > 3 ? kRingBytes : 16];
         char *const ring0 = first_ring();
         __shared__ __attribute__((aligned(16))) uint8_t scales0[Mul::kScaled ? kScaleBytes * H : 16], scales1[Mul::kScaled ? kScaleBytes * H : 16];
         typedef StageLoads<XT, XS, kThreads, H, EDGE> LoadsX;
@@ -459,12 +459,10 @@ struct TileProduct {
 #pragma unroll
             for (int slice = 0; slice < kSlices; ++slice) load(ring, slice);
         };
-        load_all(ring0);
-        if constexpr (R > 2) {
-            load_all(ring1);
-            load_all(ring2);
-        }
-        load(R > 2 ? ring3 : ring1, 0);
+        auto ring = [&](int i) { return i == 0 ? ring0 : i == 1 ? ring1 : i == 2 ? ring2 : ring3; };
+#pragma unroll
+        for (int i = 0; i < R - 1; ++i) load_all(ring(i));
+        load(ring(R - 1), 0);
         if constexpr (Mul::kScaled) {
             write_scales(scales0, scales_at[0]);
             write_scales(scales1, scales_at[1]);
@@ -501,19 +499,12 @@ struct TileProduct {
             }
             if constexpr (Mul::kScaled) scales = scales_next;
         };
-        for (int s = 0; s < stages; s += R) {
-            if constexpr (R == 2) {
-                stage(ring0, ring1, ring1, scales0, scales1, 0, s);
-                if (s + 1 >= stages) break;
-                stage(ring1, ring0, ring0, scales1, scales0, 1, s + 1);
-            } else {
-                stage(ring0, ring1, ring3, scales0, scales1, 0, s);
-                if (s + 1 >= stages) break;
-                stage(ring1, ring2, ring0, scales1, scales0, 1, s + 1);
-                if (s + 2 >= stages) break;
-                stage(ring2, ring3, ring1, scales0, scales1, 0, s + 2);
-                if (s + 3 >= stages) break;
-                stage(ring3, ring0, ring2, scales1, scales0, 1, s + 3);
+        constexpr int kTurn = R % 2 ? 2 * R : R;          // stages after which ring and parity are where they were
+        for (int s = 0; s < stages; s += kTurn) {
+#pragma unroll
+            for (int u = 0; u < kTurn; ++u) {
+                if (u && s + u >= stages) break;
+                stage(ring(u % R), ring((u + 1) % R), ring((u + R - 1) % R), u & 1 ? scales1 : scales0, u & 1 ? scales0 : scales1, u & 1, s + u);
             }
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);     // nothing is on its way to LDS any more
@@ -590,38 +581,44 @@ __device__ __forceinline__ void tile_of_block(int block, int tiles_x, int tiles_
     tx = in / high;
 }
 
-// Tiles of the products.  What a tile's side costs in the efficiency of the matrix cores it gains where there are few tiles: measured on
-// large products 256 x 256 reaches 1170 to 1330 TFLOP/s, 128 x 128 820 to 1120; 8192 rows of the smaller one's blocks, two to a compute
-// unit, take 1.4 times as long as the larger's for the same work.
-enum TileSize { kTileLarge, kTileMiddle, kTileFew, kTileFewest };
+// Tiles of the products, and how many of their blocks a compute unit has at a time.
+enum TileSize { kTileLarge, kTileHalf, kTileMiddle, kTileFew, kTileFewest };
 struct TileDims {
     int x, y;
 };
-// x by y results a tile.  float32 in parts takes three times the room in LDS, and tiles half as high.  The last: 64 by 16 rows, of 128
-// columns where x is stored across k.
+// x by y results a tile.  float32 in parts takes three times the room in LDS, and tiles half as high (and no half ones).  The last: 64 by
+// 16 rows, of 128 columns where x is stored across k.
 constexpr TileDims dims_of(TileSize s, bool parts, bool across)
 {
-    return s == kTileLarge ? TileDims{256, parts ? 128 : 256} : s == kTileMiddle ? TileDims{128, parts ? 64 : 128} : s == kTileFew ? TileDims{64, 64} : TileDims{across ? 128 : 64, 16};
+    return s == kTileLarge ? TileDims{256, parts ? 128 : 256} : s == kTileHalf ? TileDims{256, 128} : s == kTileMiddle ? TileDims{128, parts ? 64 : 128} :
+           s == kTileFew ? TileDims{64, 64} : TileDims{across ? 128 : 64, 16};
 }
 inline int64_t tiles_of(int64_t x, int64_t y, TileDims t) { return (x + t.x - 1) / t.x * ((y + t.y - 1) / t.y); }
 
-// The larger tile, unless the rounds its blocks take on 256 compute units are so much emptier than the smaller's, two to a compute unit, that
-// those are faster.
-inline TileSize tile_for(int64_t x, int64_t y, bool parts)
+// The tile that is through first, of large ones (one block to a compute unit, 256 of which take 1), half ones and middle ones (two; where 256
+// or fewer are left over, each has a compute unit to itself and takes 0.6 as long).  Measured on large products in bfloat16: 512 half ones take
+// 1.1 (operands along k: 8192 x 47236 x 4096 in 2.81 and 3.10 ms), both operands across k 0.93 (47236 x 4096 x 8192 in 2.46 and 2.29 ms),
+// 512 middle ones 0.7 for their half of the work.
+inline TileSize tile_for(int64_t x, int64_t y, bool parts, bool half, bool across)
 {
-    const int64_t large = tiles_of(x, y, dims_of(kTileLarge, parts, false)), middle = tiles_of(x, y, dims_of(kTileMiddle, parts, false));
-    return 1.4 * 0.5 * static_cast<double>((middle + 511) / 512) < static_cast<double>((large + 255) / 256) ? kTileMiddle : kTileLarge;
+    auto pairs = [](int64_t tiles, double each) { return each * (static_cast<double>(tiles / 512) + (tiles % 512 > 256 ? 1.0 : tiles % 512 ? 0.6 : 0.0)); };
+    const double large = static_cast<double>((tiles_of(x, y, dims_of(kTileLarge, parts, across)) + 255) / 256);
+    const double halves = half && !parts ? pairs(tiles_of(x, y, dims_of(kTileHalf, parts, across)), across ? 0.93 : 1.1) : large;
+    const double middle = pairs(tiles_of(x, y, dims_of(kTileMiddle, parts, across)), 0.7);
+    return middle < large && middle < halves ? kTileMiddle : halves < large ? kTileHalf : kTileLarge;
 }
 // ... of products over `rows` rows.
-inline TileSize tile_for_rows(int64_t x, int64_t rows, bool parts)
+inline TileSize tile_for_rows(int64_t x, int64_t rows, bool parts, bool half)
 {
-    return rows <= 16 ? kTileFewest : rows <= 64 ? kTileFew : tile_for(x, rows, parts);
+    return rows <= 16 ? kTileFewest : rows <= 64 ? kTileFew : tile_for(x, rows, parts, half, false);
 }
 
-// kernel<what, x, y, WX, WY, H, R, P> in a tile's size: its wavefronts, steps a stage, stages in the ring, parts of a number.
-#define DQ_TILE_CASE(kernel, what, parts, size, few, launch, ...)                                                              \
+// kernel<what, x, y, WX, WY, H, R, P> in a tile's size: its wavefronts, steps a stage, stages in the ring, parts of a number.  half, few: the
+// kernels of half tiles and of the smallest.
+#define DQ_TILE_CASE(kernel, what, parts, size, half, few, launch, ...)                                                        \
     switch (size) {                                                                                                            \
     case kTileLarge: kernel<what, 256, parts ? 128 : 256, 2, 4, 1, parts ? 2 : 4, parts ? 3 : 1><<<launch(512)>>>(__VA_ARGS__); break;     \
+    case kTileHalf: half<<<launch(256)>>>(__VA_ARGS__); break;                                                                 \
     case kTileMiddle: kernel<what, 128, parts ? 64 : 128, 2, 2, 1, parts ? 2 : 4, parts ? 3 : 1><<<launch(256)>>>(__VA_ARGS__); break;     \
     case kTileFew: kernel<what, 64, 64, 2, 2, parts ? 1 : 2, 4, parts ? 3 : 1><<<launch(256)>>>(__VA_ARGS__); break;          \
     case kTileFewest: few<<<launch(256)>>>(__VA_ARGS__); break;                                                                \

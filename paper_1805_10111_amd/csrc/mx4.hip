@@ -218,13 +218,13 @@ static int32_t dequantize4(const dq_mx4 &q, void *out, int64_t ld, hipStream_t s
 template <int TYPE>
 static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int64_t ld, hipStream_t st)
 {
-    const TileSize size = tile_for_rows(w.n, a.n, false);
+    const TileSize size = tile_for_rows(w.n, a.n, false, false);
     const TileDims t = dims_of(size, false, false);
     const int64_t tiles_x = (w.n + t.x - 1) / t.x, tiles_y = (a.n + t.y - 1) / t.y;
     if (tiles_x * tiles_y > kMost4) return DQ_ERR_UNSUPPORTED;
     auto operand = [](const dq_mx4 &q) { return Operand{reinterpret_cast<const char *>(q.codes), q.ld_codes, q.n, static_cast<int32_t>(groups_of(q.d) * 32), 0, q.scales, q.ld_scales}; };
 #define DQ_GRID(threads) static_cast<unsigned>(tiles_x * tiles_y), threads, 0, st
-    DQ_TILE_CASE(mx4_product_kernel, TYPE, false, size, (mx4_product_kernel<TYPE, 64, 16, 4, 1, 2, 4, 1>), DQ_GRID, operand(w), operand(a), groups_of(a.d) * 32,
+    DQ_TILE_CASE(mx4_product_kernel, TYPE, false, size, (mx4_product_kernel<TYPE, 128, 128, 2, 2, 1, 4, 1>), (mx4_product_kernel<TYPE, 64, 16, 4, 1, 2, 4, 1>), DQ_GRID, operand(w), operand(a), groups_of(a.d) * 32,
                  static_cast<int>(tiles_x), static_cast<int>(tiles_y), static_cast<typename Num<TYPE>::Mem *>(out), ld)
 #undef DQ_GRID
     DQ_LAUNCH_CHECK();
