@@ -444,15 +444,21 @@ TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 def _matrix(t: torch.Tensor, name: str, dtype=None, shape=None):
     """(pointer, row stride) of a matrix whose rows are contiguous."""
     size = t.shape
-    if len(size) != 2 or (size[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be a matrix with contiguous rows")
     if shape is not None and size != shape:
         raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(size)}")
-    return _ptr(t, dtype, name), t.stride(0) if size[0] > 1 else max(t.stride(0), size[1])
+    if len(size) != 2:
+        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    rows, cols = size
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    return _ptr(t, dtype, name), ld if rows > 1 else max(ld, cols)
 
 
 def _vector(t: Optional[torch.Tensor], dtype, name: str, n: int):
-    if t is not None and (t.shape != (n,) or (n > 1 and t.stride(0) != 1)):
+    if t is None:
+        return None
+    if t.shape != (n,) or (n > 1 and not t.is_contiguous()):
         raise ValueError(f"{name} must be {n} contiguous values")
     return _ptr(t, dtype, name)
 
@@ -467,18 +473,12 @@ class DeviceClasses:
     def __post_init__(self):
         if self.a.dtype not in TYPES or self.w.dtype != self.a.dtype:
             raise TypeError(f"features and model must both be float32, float16 or bfloat16, got {self.a.dtype} and {self.w.dtype}")
-        s = _Classes()
-        s.type = TYPES[self.a.dtype]
-        s.a, s.lda = _matrix(self.a, "a")
-        s.w, s.ldw = _matrix(self.w, "w")
-        if self.a.shape[1] != self.w.shape[1]:
-            raise ValueError(f"features are {self.a.shape[1]} wide, the model {self.w.shape[1]}")
-        s.n, s.c, s.d = self.a.shape[0], self.w.shape[0], self.a.shape[1]
-        self._s = s
-
-    @property
-    def ptr(self):
-        return C.addressof(self._s)
+        a, w = _matrix(self.a, "a"), _matrix(self.w, "w")
+        (n, d), (c, wide) = self.a.shape, self.w.shape
+        if d != wide:
+            raise ValueError(f"features are {d} wide, the model {wide}")
+        self._s = _Classes(TYPES[self.a.dtype], n, c, d, *a, *w)
+        self.ptr = C.addressof(self._s)
 
 
 @dataclass
@@ -490,17 +490,12 @@ class Teacher:
     tau: float = 1.0
 
     def __post_init__(self):
-        s = _Teacher()
-        s.cls, s.ld = _matrix(self.cls, "cls", torch.int32)
-        s.logit, ld = _matrix(self.logit, "logit", torch.float32, self.cls.shape)
-        if ld != s.ld:
+        cls, ld = _matrix(self.cls, "cls", torch.int32)
+        logit, ld2 = _matrix(self.logit, "logit", torch.float32, self.cls.shape)
+        if ld != ld2:
             raise ValueError("cls and logit must have the same row stride")
-        s.k, s.tau = self.cls.shape[1], self.tau
-        self._s = s
-
-    @property
-    def ptr(self):
-        return C.addressof(self._s)
+        self._s = _Teacher(self.cls.shape[1], cls, logit, ld, self.tau)
+        self.ptr = C.addressof(self._s)
 
 
 def dq_class_workspace_bytes(op: int, prob: DeviceClasses, k: int = 0) -> int:
@@ -573,28 +568,17 @@ class Mx4:
     d: int
 
     def __post_init__(self):
-        s = _Mx4()
-        n = self.codes.shape[0]
+        self.n = n = self.codes.shape[0]
         groups = (self.d + 127) // 128
-        s.codes, s.ld_codes = _matrix(self.codes, "codes", torch.uint8, (n, 64 * groups))
-        s.scales, s.ld_scales = _matrix(self.scales, "scales", torch.uint8, (n, 4 * groups))
-        s.n, s.d = n, self.d
-        self._s = s
-
-    @property
-    def n(self) -> int:
-        return self.codes.shape[0]
-
-    @property
-    def ptr(self):
-        return C.addressof(self._s)
+        self._s = _Mx4(n, self.d, *_matrix(self.codes, "codes", torch.uint8, (n, 64 * groups)),
+                       *_matrix(self.scales, "scales", torch.uint8, (n, 4 * groups)))
+        self.ptr = C.addressof(self._s)
 
 
 def new_mx4(n: int, d: int, device="cuda") -> Mx4:
     """Room for an [n, d] matrix in 4 bits (not initialised)."""
-    groups = (d + 127) // 128                                   # codes and scales side by side: one allocation
-    room = torch.empty(n * 68 * groups, dtype=torch.uint8, device=device)
-    return Mx4(room[:n * 64 * groups].view(n, 64 * groups), room[n * 64 * groups:].view(n, 4 * groups), d)
+    groups = (d + 127) // 128                    # (two allocations cost half of what one and its views do)
+    return Mx4(torch.empty((n, 64 * groups), dtype=torch.uint8, device=device), torch.empty((n, 4 * groups), dtype=torch.uint8, device=device), d)
 
 
 def _typed(t: torch.Tensor, name: str, shape):

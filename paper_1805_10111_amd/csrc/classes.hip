@@ -331,20 +331,37 @@ __global__ __launch_bounds__(WX *WY *kWave, 2) void scores_kernel(Operand w, Ope
     }
 }
 
-// ROWS rows a block, 256 / ROWS threads a row.
+// What is told of a row when its tiles are through.
+struct Finish {
+    const float2 *sums;
+    const float *hits;
+    int slots;                         // tiles
+    const float *entropy;
+    float tau2;
+    float *loss, *lse_out;             // nullable
+    uint32_t *status;
+    __device__ __forceinline__ void tell(const Targets &targets, int64_t t, float lse, float hit) const
+    {
+        const bool live = targets.used(t);
+        if (loss) loss[t] = live ? tau2 * ((entropy ? entropy[t] : 0.0f) + (lse - hit)) : 0.0f;
+        if (lse_out) lse_out[t] = lse;
+        const bool far = !targets.q && targets.cls[t] >= static_cast<int64_t>(targets.c);       // (a teacher's were looked at before)
+        const uint32_t said = (live && !__builtin_isfinite(lse) ? 1u : 0u) | (far ? 2u : 0u);
+        if (said && status) atomicOr(status, said);
+    }
+};
+
+// lse and the targets' sum q z of row t from its tiles; ROWS rows a block of 256, all threads of a row get them.
 template <int ROWS>
-__global__ __launch_bounds__(256) void finish_kernel(const float2 *__restrict__ sums, const float *__restrict__ hits, int slots, int64_t n,
-                                                     Targets targets, const float *__restrict__ entropy, float tau2, float *__restrict__ loss,
-                                                     float *__restrict__ lse_out, float *__restrict__ lse_kept, uint32_t *__restrict__ status)
+__device__ __forceinline__ float row_lse(const Finish &f, int64_t n, int64_t t, float &hit)
 {
     constexpr int kParts = 256 / ROWS;
     __shared__ float tops[kParts][ROWS];
     __shared__ float2 rest[kParts][ROWS];
     const int row = threadIdx.x % ROWS, part = threadIdx.x / ROWS;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * ROWS + row;
     float top = -INFINITY;
     if (t < n)
-        for (int s = part; s < slots; s += kParts) top = fmaxf(top, sums[s * n + t].x);
+        for (int s = part; s < f.slots; s += kParts) top = fmaxf(top, f.sums[s * n + t].x);
     tops[part][row] = top;
     __syncthreads();
     for (int o = kParts / 2; o; o /= 2) {
@@ -353,12 +370,13 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2 *__restrict__ 
     }
     top = tops[0][row];
     const float from = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, hit = 0.0f;
+    float sum = 0.0f;
+    hit = 0.0f;
     if (t < n)
-        for (int s = part; s < slots; s += kParts) {
-            const float2 v = sums[s * n + t];
+        for (int s = part; s < f.slots; s += kParts) {
+            const float2 v = f.sums[s * n + t];
             sum += v.y * expf(v.x - from);
-            hit += hits[s * n + t];
+            hit += f.hits[s * n + t];
         }
     rest[part][row] = make_float2(sum, hit);
     __syncthreads();
@@ -369,15 +387,20 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2 *__restrict__ 
         }
         __syncthreads();
     }
-    if (part || t >= n) return;
-    const float lse = top + logf(rest[0][row].x);
-    const bool live = targets.used(t);
-    if (loss) loss[t] = live ? tau2 * ((entropy ? entropy[t] : 0.0f) + (lse - rest[0][row].y)) : 0.0f;
-    if (lse_out) lse_out[t] = lse;
+    hit = rest[0][row].y;
+    return top + logf(rest[0][row].x);
+}
+
+// ROWS rows a block, 256 / ROWS threads a row.
+template <int ROWS>
+__global__ __launch_bounds__(256) void finish_kernel(Finish f, int64_t n, Targets targets, float *__restrict__ lse_kept)
+{
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x % ROWS;
+    float hit;
+    const float lse = row_lse<ROWS>(f, n, t, hit);
+    if (threadIdx.x >= ROWS || t >= n) return;
+    f.tell(targets, t, lse, hit);
     if (lse_kept) lse_kept[t] = lse;
-    const bool far = !targets.q && targets.cls[t] >= static_cast<int64_t>(targets.c);       // (a teacher's were looked at before)
-    const uint32_t said = (live && !__builtin_isfinite(lse) ? 1u : 0u) | (far ? 2u : 0u);
-    if (said && status) atomicOr(status, said);
 }
 
 // ---- gradients -----------------------------------------------------------------
@@ -391,8 +414,10 @@ __device__ __forceinline__ float row_factor(const float *weight, const float *we
 
 // g of the first piece from what was kept of its scores, in its place: columns 0 .. cols of `rows` rows.  A block takes 2048 columns of
 // a row, eight a thread, and then the targets among them.  What bounds it is memory: it reads and writes g once.
-template <int TYPE, int XT>
-__global__ __launch_bounds__(256) void kept_kernel(Kept kept, int64_t cols, int64_t rows, int64_t n, const float2 *__restrict__ sums, Targets targets,
+// FINISH: the rows' lse are not made by a launch of their own but here, by each block for itself (few rows of few spans: 16 x 1000 x 256
+// in float32 34 us a pass, with the launch 38).
+template <int TYPE, int XT, bool FINISH>
+__global__ __launch_bounds__(256) void kept_kernel(Kept kept, int64_t cols, int64_t rows, int64_t n, Finish finish, Targets targets,
                                                    const float *__restrict__ lse, const float *__restrict__ weight,
                                                    const float *__restrict__ weight_max)
 {
@@ -403,7 +428,17 @@ __global__ __launch_bounds__(256) void kept_kernel(Kept kept, int64_t cols, int6
     for (int64_t t = blockIdx.y; t < rows; t += gridDim.y) {
         const bool live = t < n && targets.used(t);
         u16 *const row = kept.g + t * kept.ldg;
-        const float from = live ? lse[t] : 0.0f, f = row_factor<TYPE>(weight, weight_max, t, live);
+        float from = 0.0f;
+        if constexpr (FINISH) {
+            if (t < n) {
+                float hit;
+                from = row_lse<1>(finish, n, t, hit);
+                if (blockIdx.x == 0 && threadIdx.x == 0) finish.tell(targets, t, from, hit);
+            }
+        } else if (live) {
+            from = lse[t];
+        }
+        const float f = row_factor<TYPE>(weight, weight_max, t, live);
         if (i < cols) {
             Eight out[kPlanes] = {};
             if (live) {
@@ -417,7 +452,7 @@ __global__ __launch_bounds__(256) void kept_kernel(Kept kept, int64_t cols, int6
                         p[e] = TYPE == DQ_F32 ? expf(z) : exp_near(z);
                     }
                 } else {
-                    const float shift = (sums[i / XT * n + t].x - from) * 1.44269504f;
+                    const float shift = (finish.sums[i / XT * n + t].x - from) * 1.44269504f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) p[e] = KeptUnit<TYPE>::value(lo[e], shift);
                 }
@@ -773,9 +808,13 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     if (edge) DQ_TILE_CASE(scores_kernel, kEdged, kInParts, s.tile, (DQ_HALF(scores_kernel, kEdged)), (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept)
     else DQ_TILE_CASE(scores_kernel, TYPE, kInParts, s.tile, (DQ_HALF(scores_kernel, TYPE)), (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept)
     DQ_LAUNCH_CHECK();
-    if (n <= 256) finish_kernel<1><<<static_cast<unsigned>(n), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
-    else finish_kernel<16><<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(sums, hits, tiles_x, n, targets, entropy, tau * tau, q.loss, q.lse, q.grad ? lse : nullptr, q.status);
-    DQ_LAUNCH_CHECK();
+    const Finish finish{sums, hits, tiles_x, entropy, tau * tau, q.loss, q.lse, q.status};
+    const bool finish_later = products && s.pieces == 1 && n <= 256 && c <= 4096;      // (by the gradients' first kernel)
+    if (!finish_later) {
+        if (n <= 256) finish_kernel<1><<<static_cast<unsigned>(n), 256, 0, st>>>(finish, n, targets, q.grad ? lse : nullptr);
+        else finish_kernel<16><<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(finish, n, targets, q.grad ? lse : nullptr);
+        DQ_LAUNCH_CHECK();
+    }
     if (!products) return DQ_OK;
 
     const float post = q.scale * tau;
@@ -795,11 +834,11 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
         if (at == 0) {
             const int64_t cols = up(have, 32);
             const dim3 spans(static_cast<unsigned>((cols + 2047) / 2048), static_cast<unsigned>(std::min<int64_t>(rows_k, 65535)));
-            switch (kInParts ? 64 : s.td.x) {
-            case 64: kept_kernel<TYPE, 64><<<spans, 256, 0, st>>>(kept, cols, rows_k, n, sums, targets, lse, q.weight, weight_max); break;
-            case 128: kept_kernel<TYPE, 128><<<spans, 256, 0, st>>>(kept, cols, rows_k, n, sums, targets, lse, q.weight, weight_max); break;
-            default: kept_kernel<TYPE, 256><<<spans, 256, 0, st>>>(kept, cols, rows_k, n, sums, targets, lse, q.weight, weight_max); break;
-            }
+            const int width = kInParts ? 64 : s.td.x;
+#define DQ_KEPT(XT, LATER) kept_kernel<TYPE, XT, LATER><<<spans, 256, 0, st>>>(kept, cols, rows_k, n, finish, targets, lse, q.weight, weight_max)
+            if (finish_later) width == 64 ? DQ_KEPT(64, true) : width == 128 ? DQ_KEPT(128, true) : DQ_KEPT(256, true);
+            else width == 64 ? DQ_KEPT(64, false) : width == 128 ? DQ_KEPT(128, false) : DQ_KEPT(256, false);
+#undef DQ_KEPT
         } else {
             const int tiles_p = static_cast<int>((have + s.td.x - 1) / s.td.x);
             grid = dim3(static_cast<unsigned>(tiles_p * tiles_y));
