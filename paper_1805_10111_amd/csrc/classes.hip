@@ -202,14 +202,15 @@ __global__ __launch_bounds__(kTeacherThreads) void teacher_kernel(const int32_t 
 }
 
 // ---- scores --------------------------------------------------------------------
-__device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
+__device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
 
 constexpr int kEdge = 4;               // with a type: rows that are read in place end inside of a step
 
 // The scores of the first piece stay in the place of its gradients, 16 bits of them in each plane: as they are, in two halves, in float32
-// and where there are few rows; else how far they lie below the tile's maximum, in steps of 2^-9 of a factor of two (2^-11 in float16)
-// up to a factor of 2^-128 (2^-32), behind which probabilities are zeros.  That is off by half a step, a factor of 1 -+ 0.0007
-// (0.00017): a fifth (a third) of what g's own rounding may be.  The targets' scores, where p - q may cancel, are kept whole.
+// and where there are few rows; else how far they lie below the tile's maximum, in 65535 steps up to a factor of 2^-128 (2^-32 in
+// float16), behind which probabilities are zeros.  That is off by half a step, a factor of 1 -+ 0.0007 (0.00017): a fifth (a third) of
+// what g's own rounding may be.  The targets' scores, where p - q may cancel, are kept whole.
 struct Kept {
     u16 *g;                            // null: none
     int64_t ldg, plane, cols;          // numbers; classes of the piece
@@ -218,15 +219,17 @@ struct Kept {
 constexpr bool kept_whole(int type, int x) { return type == DQ_F32 || x <= 64; }
 template <int TYPE>
 struct KeptUnit {
-    static constexpr float kSteps = TYPE == DQ_F16 ? 2048.0f : 512.0f;
-    static __device__ __forceinline__ u16 code(float top, float z)
+    static constexpr float kRange = TYPE == DQ_F16 ? 32.0f : 128.0f;
+    // two numbers, y and top being log2 of probabilities up to a common factor
+    static __device__ __forceinline__ uint32_t codes(float top, float y0, float y1)
     {
-        return static_cast<u16>(static_cast<uint32_t>(fminf((top - z) * (1.44269504f * kSteps) + 0.5f, 65535.0f)));
+        const float at = top * (1.0f / kRange);
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(__builtin_fmaf(y0, -1.0f / kRange, at), __builtin_fmaf(y1, -1.0f / kRange, at)));
     }
     // shift: log2 of exp(top - lse); a row whose lse is not a number has no number
     static __device__ __forceinline__ float value(u16 code, float shift)
     {
-        return code == 65535 && shift == shift ? 0.0f : __builtin_amdgcn_exp2f(shift - static_cast<float>(code) * (1.0f / kSteps));
+        return code == 65535 && shift == shift ? 0.0f : __builtin_amdgcn_exp2f(shift - static_cast<float>(code) * (kRange / 65535.0f));
     }
 };
 
@@ -241,66 +244,97 @@ __global__ __launch_bounds__(WX *WY *kWave, 2) void scores_kernel(Operand w, Ope
     int tx, ty;
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t c0 = static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
-    Tile tile;
-    tile.run(w, a, c0, t0, 0, k);
-    const int lane = threadIdx.x & 63, wave_c0 = static_cast<int>(c0) + Tile::sub_x(0) * 16;
+    const int wave_c0 = static_cast<int>(c0) + Tile::sub_x(0) * 16, wave_end = static_cast<int>(lesser(wave_c0 + Tile::SX * 16, c));
+    // the rows' first targets from this wavefront's classes on: looked up while the tile's first stages arrive
+    int entry[Tile::SY], at[Tile::SY];
 #pragma unroll
     for (int y = 0; y < Tile::SY; ++y) {
-        const int64_t t = t0 + Tile::at_y(y);
-        const bool live = t < n;
-        const int base = static_cast<int>(c0) + Tile::at_x(0);
-        float top = -INFINITY;
+        const int64_t t = lesser(t0 + Tile::at_y(y), n - 1);
+        entry[y] = targets.first(t, wave_c0);
+        at[y] = t0 + Tile::at_y(y) < n && entry[y] < targets.k ? targets.cls[t * targets.k + entry[y]] : kNoClass;
+    }
+    Tile tile;
+    tile.run(w, a, c0, t0, 0, k);
+    // Where what is kept is relative, scores are taken in units of a factor of two, which saves a product each.
+    constexpr bool kBits = !kept_whole(TYPE, XT);
+    const float unit = kBits ? kLn2 : 1.0f, per_unit = kBits ? inv_tau * kLog2E : inv_tau;
+    auto exp_of = [](float v) { return kBits ? __builtin_amdgcn_exp2f(v) : TYPE == DQ_F32 ? expf(v) : exp_near(v); };
+    const int lane = threadIdx.x & 63, base = static_cast<int>(c0) + Tile::at_x(0);
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y)
+#pragma unroll
+        for (int m = 0; m < Tile::SX; ++m) tile.acc[m][y] *= per_unit;
+    if (c0 + XT > c) {
+#pragma unroll
+        for (int y = 0; y < Tile::SY; ++y)
+#pragma unroll
+            for (int m = 0; m < Tile::SX; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (base + 16 * m + i >= c) tile.acc[m][y][i] = -INFINITY;
+    }
+    float top[Tile::SY], sum[Tile::SY];
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) {
+        top[y] = -INFINITY;
 #pragma unroll
         for (int m = 0; m < Tile::SX; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float z = base + 16 * m + i < c ? tile.acc[m][y][i] * inv_tau : -INFINITY;
-                tile.acc[m][y][i] = z;
-                top = fmaxf(top, z);
-            }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        float sum = 0.0f;
-        const float from = top == -INFINITY ? 0.0f : top;
+            for (int i = 0; i < 4; ++i) top[y] = fmaxf(top[y], tile.acc[m][y][i]);
+    }
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) top[y] = fmaxf(top[y], __shfl_xor(top[y], 16));
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) top[y] = fmaxf(top[y], __shfl_xor(top[y], 32));
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) {
+        const float from = top[y] == -INFINITY ? 0.0f : top[y];
+        sum[y] = 0.0f;
 #pragma unroll
         for (int m = 0; m < Tile::SX; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum += TYPE == DQ_F32 ? expf(tile.acc[m][y][i] - from) : exp_near(tile.acc[m][y][i] - from);
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
+            for (int i = 0; i < 4; ++i) sum[y] += exp_of(tile.acc[m][y][i] - from);
+    }
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) sum[y] += __shfl_xor(sum[y], 16);
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) sum[y] += __shfl_xor(sum[y], 32);
+#pragma unroll
+    for (int y = 0; y < Tile::SY; ++y) {
         float hit = 0.0f;
-        if (live) {
-            const int end = min(wave_c0 + Tile::SX * 16, static_cast<int>(c));
-            const int32_t *cls = targets.cls + t * targets.k;
-            for (int e = targets.first(t, wave_c0); e < targets.k && cls[e] < end; ++e) {
-                const int rel = cls[e] - base;
+        if (__any(at[y] < wave_end)) {
+            const int64_t t = t0 + Tile::at_y(y);
+            for (int e = entry[y], cls = at[y]; cls < wave_end;) {
+                const int rel = cls - base;
                 const float q = targets.q ? targets.q[t * targets.k + e] : 1.0f;
                 float z = 0.0f;
 #pragma unroll
                 for (int m = 0; m < Tile::SX; ++m)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) z = rel == 16 * m + i ? tile.acc[m][y][i] : z;
+                z *= unit;
                 hit += q == 0.0f ? 0.0f : q * z;
                 if (kept.target_z && rel >= 0 && rel < Tile::SX * 16 && (rel & 15) < 4) kept.target_z[t * targets.k + e] = z;
+                cls = ++e < targets.k ? targets.cls[t * targets.k + e] : kNoClass;
             }
+            hit += __shfl_xor(hit, 16);
+            hit += __shfl_xor(hit, 32);
         }
-        hit += __shfl_xor(hit, 16);
-        hit += __shfl_xor(hit, 32);
-        if (lane < 16) shared[Tile::wave() % WX][Tile::at_y(y)] = make_float3(top, sum, hit);
+        if (lane < 16) shared[Tile::wave() % WX][Tile::at_y(y)] = make_float3(top[y], sum[y], hit);
     }
     __syncthreads();
     for (int r = threadIdx.x; r < YT && t0 + r < n; r += WX * WY * kWave) {
-        float top = -INFINITY, sum = 0.0f, hit = 0.0f;
+        float all = -INFINITY, total = 0.0f, hit = 0.0f;
 #pragma unroll
-        for (int x = 0; x < WX; ++x) top = fmaxf(top, shared[x][r].x);
-        const float from = top == -INFINITY ? 0.0f : top;
+        for (int x = 0; x < WX; ++x) all = fmaxf(all, shared[x][r].x);
+        const float from = all == -INFINITY ? 0.0f : all;
 #pragma unroll
         for (int x = 0; x < WX; ++x) {
             const float3 v = shared[x][r];
-            sum += v.y * expf(v.x - from);
+            total += v.y * exp_of(v.x - from);
             hit += v.z;
         }
-        sums[static_cast<int64_t>(tx) * n + t0 + r] = make_float2(top, sum);
+        sums[static_cast<int64_t>(tx) * n + t0 + r] = make_float2(all * unit, total);
         hits[static_cast<int64_t>(tx) * n + t0 + r] = hit;
     }
     if (!kept.g || c0 >= kept.cols) return;
@@ -315,18 +349,14 @@ __global__ __launch_bounds__(WX *WY *kWave, 2) void scores_kernel(Operand w, Ope
                 return r;
             });
     } else {
-        float top[Tile::SY];
 #pragma unroll
-        for (int y = 0; y < Tile::SY; ++y) {
-            top[y] = -INFINITY;
+        for (int y = 0; y < Tile::SY; ++y)
 #pragma unroll
             for (int x = 0; x < WX; ++x) top[y] = fmaxf(top[y], shared[x][Tile::at_y(y)].x);
-        }
         tile.store(to, kept.ldg, YT, XT, [&](int m, int y) {
-            u16x4 r;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = KeptUnit<TYPE>::code(top[y], tile.acc[m][y][i]);
-            return r;
+            const f32x4 v = tile.acc[m][y];
+            typedef __attribute__((ext_vector_type(2))) uint32_t Two;
+            return __builtin_bit_cast(u16x4, Two{KeptUnit<TYPE>::codes(top[y], v[0], v[1]), KeptUnit<TYPE>::codes(top[y], v[2], v[3])});
         });
     }
 }
@@ -452,7 +482,7 @@ __global__ __launch_bounds__(256) void kept_kernel(Kept kept, int64_t cols, int6
                         p[e] = TYPE == DQ_F32 ? expf(z) : exp_near(z);
                     }
                 } else {
-                    const float shift = (finish.sums[i / XT * n + t].x - from) * 1.44269504f;
+                    const float shift = (finish.sums[i / XT * n + t].x - from) * kLog2E;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) p[e] = KeptUnit<TYPE>::value(lo[e], shift);
                 }
