@@ -249,7 +249,8 @@ struct TileProduct {
     static __device__ __forceinline__ int at_y(int n) { return sub_y(n) * 16 + (threadIdx.x & 15); }
 
     // Scales of 4-bit numbers.  A step has four blocks a row; LDS holds their scales as [block][row % 16][row / 16], so that what a
-    // lane needs for its subtiles are neighbouring bytes.  Thread r brings those of row r (x's rows, then y's).
+    // lane needs for its subtiles are neighbouring bytes.  Thread r brings those of row r (x's rows, then y's): where a stage is one step,
+    // of four stages at a time, 16 bytes (each thread's row is a line of its own in the cache, and a line a stage took as long as the codes).
     static constexpr int kScaleBytes = 4 * (XT + YT);       // of a step
     static_assert(!Mul::kScaled || XT + YT <= kThreads, "a thread brings one row's scales");
     struct Scales {
@@ -282,11 +283,30 @@ struct TileProduct {
         for (int h = 0; h < H; ++h) b.v[h] = row ? *reinterpret_cast<const uint32_t *>(row + lesser(stage * H + h, groups - 1) * 4) : 0;
         return b;
     }
+    // Those of stages `stage` to stage + 3, or of the row's last four.
+    static __device__ __forceinline__ i32x4 load_four(const uint8_t *row, int stage, int groups)
+    {
+        struct __attribute__((packed, aligned(4))) Four {
+            i32x4 v;
+        };
+        return reinterpret_cast<const Four *>(row + max(min(stage, groups - 4), 0) * 4)->v;
+    }
+    // Stage s + i's of those of stage s on (behind the last, where codes are zeros: any).
+    static __device__ __forceinline__ Brought one_of(const i32x4 &four, int s, int i, int groups)
+    {
+        const int past = s - (groups - 4);                       // stages of the row's last four that came before s
+        uint32_t v = static_cast<uint32_t>(four[i]);
+#pragma unroll
+        for (int by = 1; by + i < 4; ++by) v = past == by ? static_cast<uint32_t>(four[i + by]) : v;
+        Brought b{};
+        b.v[0] = v;
+        return b;
+    }
     static __device__ __forceinline__ void write_scales(uint8_t *lds, const Brought &b)
     {
         const bool in_x = threadIdx.x < XT;
         const int r = in_x ? threadIdx.x : threadIdx.x - XT, rows = in_x ? XT : YT;
-        if (r >= rows) return;
+        if (XT + YT < kThreads && r >= rows) return;
         uint8_t *const at = lds + (in_x ? 0 : 4 * XT) + (r & 15) * (rows / 16) + (r >> 4);
 #pragma unroll
         for (int h = 0; h < H; ++h)
@@ -353,8 +373,8 @@ struct TileProduct {
 
     // Stores the tile row by row j, value(m, n) the four results of subtile (m, n) in memory's type: out: where the tile's first row
     // begins, rows, cols: how many of the tile's rows and of their columns there are.  A lane's four results are 8 or 16 bytes of one of sixteen
-    // rows; each wavefront turns them, through its part of LDS, into up to 256 neighbouring bytes of a row.  (Scores of 8192 x 47236
-    // classes: written four at a time 1290 us, so ___ us.)
+    // rows; each wavefront turns them, through its part of LDS, into up to 256 neighbouring bytes of a row.  (The
+    // gradient of a 20011 x 1001 float16 model: written four numbers at a time 83 us, so 50.)
     template <class Mem, class Value>
     __device__ __forceinline__ void store(Mem *out, int64_t ld, int64_t rows, int64_t cols, Value value) const
     {
@@ -447,7 +467,22 @@ struct TileProduct {
         Brought brought[2] = {}, scales_at[2] = {};      // scales on their way to LDS, by the stage; of the first two stages
         const uint8_t *row = nullptr;
         const int64_t groups = k1 / 32;
-        if constexpr (Mul::kScaled) {
+        i32x4 four{}, four_next{};              // of this turn of the ring's stages and of the next
+        constexpr bool kFours = Mul::kScaled && H == 1;
+        static_assert(!kFours || (R == 4 && XT + YT == kThreads), "a turn is four stages, every thread has a row");
+        if constexpr (kFours) {
+            const int t = threadIdx.x;
+            row = t < XT ? x.scales + lesser(i0 + t, x.rows - 1) * x.ld_scales : y.scales + lesser(j0 + t - XT, y.rows - 1) * y.ld_scales;
+            if (groups >= 4) {
+                four = load_four(row, 0, static_cast<int>(groups));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) four[i] = *reinterpret_cast<const int *>(row + min(i, static_cast<int>(groups) - 1) * 4);
+                row = reinterpret_cast<const uint8_t *>(x.p);       // (for the loop, which asks for a next turn's without a branch: some 16 bytes)
+            }
+            scales_at[0].v[0] = four[0];
+            scales_at[1].v[0] = four[1];
+        } else if constexpr (Mul::kScaled) {
             const int t = threadIdx.x;
             row = t < XT ? x.scales + lesser(i0 + t, x.rows - 1) * x.ld_scales : t < XT + YT ? y.scales + lesser(j0 + t - XT, y.rows - 1) * y.ld_scales : nullptr;
             scales_at[0] = load_scales(row, 0, groups);
@@ -473,7 +508,8 @@ struct TileProduct {
         read_part(ring0, 0, px[0], py[0]);
         if constexpr (Mul::kScaled) read_scales(scales0, scales);
         // Stage s out of `now`; `next` holds the next one, the second slice of `later` is still to be asked for.
-        auto stage = [&](char *now, char *next, char *later, uint8_t *ss, uint8_t *sn, int parity, int s) {
+        auto stage = [&](char *now, char *next, char *later, uint8_t *ss, uint8_t *sn, int u, int s) {
+            const int parity = u & 1;
             constexpr int kPerX = P * (XS ? 2 : 1), kPerY = P * (YS ? 2 : 1), kProducts = (P > 1 ? kPartProducts : 1) * kQ * SY;
 #pragma unroll
             for (int part = 0; part < kParts; ++part) {
@@ -487,8 +523,17 @@ struct TileProduct {
                     stage_arrived<(R - 2) * kEach>();                    // the next stage's; what was asked for since then is on its way
                     if constexpr (Mul::kScaled) {
                         read_scales(sn, scales_next);                    // written before this barrier
-                        write_scales(ss, brought[parity]);               // stage s + 2's; what was there was read before it
-                        brought[parity] = load_scales(row, s + 4, groups);
+                        // stage s + 2's; what was there was read before it
+                        if constexpr (kFours) {
+                            const int turn = s - u;
+                            const int most = max(static_cast<int>(groups), 4);
+                            write_scales(ss, u < 2 ? one_of(four, turn, (u + 2) & 3, most) : one_of(four_next, turn + 4, (u + 2) & 3, most));
+                            if (u == 0) four_next = load_four(row, turn + 4, static_cast<int>(groups));
+                            if (u == 3) four = four_next;
+                        } else {
+                            write_scales(ss, brought[parity]);
+                            brought[parity] = load_scales(row, s + 4, groups);
+                        }
                     }
                     read_part(next, 0, px[mine ^ 1], py[y_next]);        // (after the last stage: zeros)
                     load(now, 0);
@@ -500,12 +545,20 @@ struct TileProduct {
             if constexpr (Mul::kScaled) scales = scales_next;
         };
         constexpr int kTurn = R % 2 ? 2 * R : R;          // stages after which ring and parity are where they were
-        for (int s = 0; s < stages; s += kTurn) {
+        auto step = [&](int u, int s) {
+            stage(ring(u % R), ring((u + 1) % R), ring((u + R - 1) % R), u & 1 ? scales1 : scales0, u & 1 ? scales0 : scales1, u, s + u);
+        };
+        // (Whole turns in a loop without exits: with them the compiler loses track of what has arrived where the loop begins again, and waits
+        // there for all but one of the loads: 8192 x 47236 x 4096 in bfloat16 2.65 ms for its scores instead of 2.75.)
+        int s = 0;
+        for (; s + kTurn <= stages; s += kTurn) {
 #pragma unroll
-            for (int u = 0; u < kTurn; ++u) {
-                if (u && s + u >= stages) break;
-                stage(ring(u % R), ring((u + 1) % R), ring((u + R - 1) % R), u & 1 ? scales1 : scales0, u & 1 ? scales0 : scales1, u & 1, s + u);
-            }
+            for (int u = 0; u < kTurn; ++u) step(u, s);
+        }
+#pragma unroll
+        for (int u = 0; u < kTurn - 1; ++u) {
+            if (s + u >= stages) break;
+            step(u, s);
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);     // nothing is on its way to LDS any more
     }
