@@ -63,7 +63,6 @@ struct Packed {
     int64_t ld, rows, cols;
     u16 *out, *used;                   // either may be null
     int64_t out_rows, used_rows;       // with the zeros behind them
-    int vector;                        // rows that can be read 16 bytes at a time
 };
 template <int TYPE>
 __device__ __forceinline__ void pack_eight(const Packed &j, int64_t out_cols, int64_t i, const Targets &targets)
@@ -74,14 +73,13 @@ __device__ __forceinline__ void pack_eight(const Packed &j, int64_t out_cols, in
     u16 part[3][8];
     Mem x[8] = {};
     if (r < j.rows) {
-        if (j.vector && c + 8 <= j.cols) {
-            typedef __attribute__((ext_vector_type(16 / sizeof(Mem)))) Mem Wide;
+        if (c + 8 <= j.cols) {                       // (16-byte loads of any alignment to the number)
+            struct __attribute__((packed, aligned(sizeof(Mem)))) All {
+                __attribute__((ext_vector_type(8))) Mem v;
+            };
+            const All all = *reinterpret_cast<const All *>(row + c);
 #pragma unroll
-            for (int h = 0; h < static_cast<int>(sizeof(Mem)) / 2; ++h) {
-                const Wide w = *reinterpret_cast<const Wide *>(row + c + h * (16 / sizeof(Mem)));
-#pragma unroll
-                for (int e = 0; e < static_cast<int>(16 / sizeof(Mem)); ++e) x[h * (16 / sizeof(Mem)) + e] = w[e];
-            }
+            for (int e = 0; e < 8; ++e) x[e] = all.v[e];
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -245,16 +243,16 @@ __global__ __launch_bounds__(WX *WY *kWave, 2) void scores_kernel(Operand w, Ope
     tile_of_block(blockIdx.x, tiles_x, tiles_y, tx, ty);
     const int64_t c0 = static_cast<int64_t>(tx) * XT, t0 = static_cast<int64_t>(ty) * YT;
     const int wave_c0 = static_cast<int>(c0) + Tile::sub_x(0) * 16, wave_end = static_cast<int>(lesser(wave_c0 + Tile::SX * 16, c));
-    // the rows' first targets from this wavefront's classes on: looked up while the tile's first stages arrive
-    int entry[Tile::SY], at[Tile::SY];
-#pragma unroll
-    for (int y = 0; y < Tile::SY; ++y) {
-        const int64_t t = lesser(t0 + Tile::at_y(y), n - 1);
-        entry[y] = targets.first(t, wave_c0);
-        at[y] = t0 + Tile::at_y(y) < n && entry[y] < targets.k ? targets.cls[t * targets.k + entry[y]] : kNoClass;
-    }
+    int entry[Tile::SY], at[Tile::SY];          // the rows' first targets from this wavefront's classes on
     Tile tile;
-    tile.run(w, a, c0, t0, 0, k);
+    tile.run(w, a, c0, t0, 0, k, [&] {
+#pragma unroll
+        for (int y = 0; y < Tile::SY; ++y) {
+            const int64_t t = lesser(t0 + Tile::at_y(y), n - 1);
+            entry[y] = targets.first(t, wave_c0);
+            at[y] = t0 + Tile::at_y(y) < n && entry[y] < targets.k ? targets.cls[t * targets.k + entry[y]] : kNoClass;
+        }
+    });
     // Where what is kept is relative, scores are taken in units of a factor of two, which saves a product each.
     constexpr bool kBits = !kept_whole(TYPE, XT);
     const float unit = kBits ? kLn2 : 1.0f, per_unit = kBits ? inv_tau * kLog2E : inv_tau;
@@ -469,6 +467,9 @@ __global__ __launch_bounds__(256) void kept_kernel(Kept kept, int64_t cols, int6
             from = lse[t];
         }
         const float f = row_factor<TYPE>(weight, weight_max, t, live);
+        // (the thread's first entry: every thread looks at its own, which is one trip to memory where a search is one for each halving)
+        const int32_t *const cls = targets.cls + t * targets.k;
+        const int e0 = static_cast<int>(threadIdx.x), mine = live && e0 < targets.k ? cls[e0] : kNoClass;
         if (i < cols) {
             Eight out[kPlanes] = {};
             if (live) {
@@ -503,20 +504,19 @@ __global__ __launch_bounds__(256) void kept_kernel(Kept kept, int64_t cols, int6
         }
         __syncthreads();
         if (!live) continue;
-        const int32_t *const cls = targets.cls + t * targets.k;
         const int end = static_cast<int>(lesser(first + 2048, kept.cols));
-        for (int e = targets.first(t, static_cast<int>(first)) + threadIdx.x; e < targets.k && cls[e] < end; e += 256) {
-            if (e && cls[e - 1] == cls[e]) continue;           // (the first of a class that comes several times takes them all)
+        for (int e = e0, j = mine; e < targets.k; e += 256, j = e < targets.k ? cls[e] : kNoClass) {
+            if (j < first || j >= end || (e && cls[e - 1] == j)) continue;           // (the first of a class that comes several times takes them all)
             const float z = kept.target_z[t * targets.k + e] - from;
             float v = TYPE == DQ_F32 ? expf(z) : exp_near(z);
-            for (int o = e; o < targets.k && cls[o] == cls[e]; ++o) v -= targets.q ? targets.q[t * targets.k + o] : 1.0f;
+            for (int o = e; o < targets.k && cls[o] == j; ++o) v -= targets.q ? targets.q[t * targets.k + o] : 1.0f;
             if constexpr (TYPE == DQ_F32) {
                 u16 part[3];
                 parts_of(f * v, part);
 #pragma unroll
-                for (int h = 0; h < 3; ++h) row[h * kept.plane + cls[e]] = part[h];
+                for (int h = 0; h < 3; ++h) row[h * kept.plane + j] = part[h];
             } else {
-                row[cls[e]] = Num<TYPE>::store(f * v);
+                row[j] = Num<TYPE>::store(f * v);
             }
         }
     }
@@ -810,10 +810,9 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     const Operand az{ws + s.az, s.dp * 2, s.rows_z, dp, s.rows_z * s.dp * 2};
     const int64_t of_a = s.direct_a && !want_dw ? 0 : (want_dw ? s.rows_z : n) * s.dp / 8, of_w = s.direct_w ? 0 : c * s.dp / 8;
     if (of_a + of_w) {
-        auto wide_rows = [&](const void *v, int64_t ld) { return aligned16(v) && ld * wide % 16 == 0; };
         const Packed pa{p.a, p.lda, n, s.d, s.direct_a ? nullptr : reinterpret_cast<u16 *>(ws + s.a), want_dw ? reinterpret_cast<u16 *>(ws + s.az) : nullptr,
-                        n, s.rows_z, wide_rows(p.a, p.lda)};
-        const Packed pw{p.w, p.ldw, c, s.d, reinterpret_cast<u16 *>(ws + s.w), nullptr, c, 0, wide_rows(p.w, p.ldw)};
+                        n, s.rows_z};
+        const Packed pw{p.w, p.ldw, c, s.d, reinterpret_cast<u16 *>(ws + s.w), nullptr, c, 0};
         const int64_t blocks = std::min<int64_t>((of_a + of_w + 255) / 256, 1 << 16);
         pack_kernel<TYPE><<<static_cast<unsigned>(blocks), 256, 0, st>>>(pa, pw, s.dp, of_a, of_a + of_w, targets);
         DQ_LAUNCH_CHECK();

@@ -363,6 +363,11 @@ struct TileProduct {
         __builtin_amdgcn_sched_group_barrier(kMatrix, PRODUCTS, 0);
     }
 
+    __device__ __forceinline__ void run(const Operand &x, const Operand &y, int64_t i0, int64_t j0, int64_t k0, int64_t k1)
+    {
+        run(x, y, i0, j0, k0, k1, [] {});
+    }
+
     static constexpr int kRingBytes = P * (XT + YT) * kStepBytes * H;
     // the first stage's memory; the results pass through it
     static __device__ __forceinline__ char *first_ring()
@@ -418,8 +423,10 @@ struct TileProduct {
             }
     }
 
-    // k0 .. k1 (in pairs of bytes, multiples of 32) of rows i0.. of x and j0.. of y.
-    __device__ __forceinline__ void run(const Operand &x, const Operand &y, int64_t i0, int64_t j0, int64_t k0, int64_t k1)
+    // k0 .. k1 (in pairs of bytes, multiples of 32) of rows i0.. of x and j0.. of y.  meanwhile(): what is done when the first stages have
+    // been asked for.
+    template <class Meanwhile>
+    __device__ __forceinline__ void run(const Operand &x, const Operand &y, int64_t i0, int64_t j0, int64_t k0, int64_t k1, Meanwhile meanwhile)
     {
         // (an array of its own for each stage: the compiler keeps apart what is read and what is arriving by the array, up to seven)
         static_assert(R >= 2 && R <= 4, "arrays for up to four stages");
@@ -498,6 +505,7 @@ struct TileProduct {
 #pragma unroll
         for (int i = 0; i < R - 1; ++i) load_all(ring(i));
         load(ring(R - 1), 0);
+        meanwhile();
         if constexpr (Mul::kScaled) {
             write_scales(scales0, scales_at[0]);
             write_scales(scales1, scales_at[1]);
