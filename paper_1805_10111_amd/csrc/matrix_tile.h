@@ -7,12 +7,14 @@
 //
 // Either operand is stored along k (row-major rows i, k contiguous), or across it (row-major rows k, i contiguous); the latter
 // reaches the matrix cores through the transposing reads of LDS, so nothing is ever transposed in memory.
-// A step is 64 bytes of k: 32 numbers of 16 bits, 128 of 4; a stage is H steps.  LDS holds a ring of four stages, filled by loads that
-// go there directly: while one is multiplied, three are on their way.  One step is right where the matrix cores bound (large tiles,
-// short stages); where memory does (few rows), rows are read 128 bytes at a time and more.
+// A step is 64 bytes of k: 32 numbers of 16 bits, 128 of 4; a stage is H steps.  LDS holds a ring of two to four stages, filled by loads
+// that go there directly: while one is multiplied, the others are on their way.  One step is right where the matrix cores bound
+// (large tiles, short stages); where memory does (few rows), rows are read 128 bytes at a time.
 //
 // What bounds it: the matrix cores.  256 x 256 with eight wavefronts (a wavefront multiplies 128 x 64: 12 reads of LDS for 32
-// products) needs 96 KB of LDS reads per 1024 cycles of matrix-core work, and each byte of memory is used for 256 products.
+// products) needs 96 KB of LDS reads per 1024 cycles of matrix-core work, which LDS does in 400, and each byte of memory is used for
+// 256 products.  A step takes 1.3 times the 1024 cycles; at 1.7 to 1.8 GHz, which is what the clocks are held to under this
+// load, that is 1470 TFLOP/s in bfloat16 (n = 8192 rows of 47236 classes times 4096 columns, where a tile is 1476 steps).
 #pragma once
 
 #include <hip/hip_bf16.h>

@@ -147,6 +147,9 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__re
     }
 }
 
+// Few rows: bound by w's codes (1 x 47236 x 4096, 103 MB, 17.7 us).  Many: 8192 x 47236 x 4096 980 us, 3230 TFLOP/s: a step is as many
+// bytes of LDS as 16-bit numbers take, with the scales to bring there, for as many cycles of the matrix cores, and takes twice these;
+// 200 us are the results' (774 MB in bfloat16).
 template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void mx4_product_kernel(Operand w, Operand a, int64_t k, int tiles_x, int tiles_y,
                                                                     typename Num<TYPE>::Mem *__restrict__ out, int64_t ld)

@@ -385,3 +385,33 @@ def test_weights_of_rows_left_out_reach_nothing(dq, t, what):
             assert torch.isfinite(got[k]).all() and (got[k] - clean[k]).abs().max() <= 2 * half_step(TYPES[t]) * clean[k].abs().max(), k
         else:
             assert torch.equal(got[k], clean[k]), k
+
+
+@pytest.mark.parametrize("t,n,c", [("bf16", 8192, 70001), ("f16", 8100, 66000), ("f32", 4096, 45000)])
+def test_classes_behind_the_piece_that_is_kept(dq, t, n, c):
+    """More classes than one piece takes: gradients from kept scores and from scores that are multiplied again."""
+    test_classes_in_several_pieces(dq, t, n, c)
+
+
+def test_teacher_over_several_pieces(dq):
+    """As above in norms; q's own error (float32) is far below the roundings of g and of the output."""
+    n, c, d, k, tau = 4096, 140000, 32, 6, 2.0
+    a, w, g = make(n, c, d, "bf16", 17)
+    cls = torch.randint(-1, c, (n, k), generator=g, dtype=torch.int32)
+    logit = 3 * torch.randn(n, k, generator=g)
+    a, w, cls, logit = a.cuda(), w.cuda(), cls.cuda(), logit.cuda()
+    got = run(dq, a, w, dq.Teacher(cls, logit, tau), None, 1.0)
+    there = cls >= 0
+    used = there.any(1)
+    q = torch.where(there, torch.exp(logit.double() / tau), 0.0)
+    q = q / q.sum(1, keepdim=True).clamp(min=1e-300)
+    z = a.double() @ w.double().T / tau
+    z -= torch.logsumexp(z, 1)[:, None]
+    ent = torch.where(q > 0, q * torch.log(q.clamp(min=1e-300)), 0.0).sum(1)
+    loss = tau * tau * (ent - (q * z.gather(1, cls.clamp(min=0).long())).sum(1)) * used
+    p = z.exp_() * used[:, None]
+    p.scatter_add_(1, cls.clamp(min=0).long(), -q)
+    p *= tau
+    for name, want in (("loss", loss), ("da", p @ w.double()), ("dw", p.mT @ a.double())):
+        bound = 1e-5 if name == "loss" else 2 * half_step(torch.bfloat16) + 2e-6
+        assert float((got[name].double() - want).norm() / want.norm()) <= bound, name

@@ -204,3 +204,16 @@ def test_in_a_graph(dq):
         call()
         torch.cuda.synchronize()
         assert torch.equal(got, out), step
+
+
+@pytest.mark.parametrize("groups", list(range(1, 14)))
+@pytest.mark.parametrize("n", [10, 150])
+def test_scores_of_any_number_of_groups(dq, n, groups):
+    """Scales are brought for four groups of 128 at a time where there are many rows: rows that end at any of them, in place of the last in memory."""
+    c, d = 200, 128 * groups - (groups % 3) * 20
+    a, w = rows(n, d, "f32", groups), rows(c, d, "f32", 50 + groups)
+    W, out = dq.new_mx4(c, d), torch.zeros(n, c, device="cuda")
+    dq.dq_mx4_quantize(w.cuda(), W)
+    dq.dq_mx4_scores(a.cuda(), W, out, None, dq.new_scores_workspace(n, d))
+    (ca, sa), (cw, sw), pad = definition(a.double().numpy()), definition(w.double().numpy()), ((0, 0), (0, -d % 32))
+    near(out, values(np.pad(ca, pad), sa, d), values(np.pad(cw, pad), sw, d), torch.float32, d)
