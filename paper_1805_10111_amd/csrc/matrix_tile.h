@@ -309,6 +309,17 @@ struct TileProduct {
         const bool in_x = threadIdx.x < XT;
         const int r = in_x ? threadIdx.x : threadIdx.x - XT, rows = in_x ? XT : YT;
         if (XT + YT < kThreads && r >= rows) return;
+        if constexpr (H == 1) {
+            // Of the 64 rows of a wavefront, rows 16 apart lie in one word: the lanes that hold them exchange bytes, and lane 16 q + j writes
+            // block q's of rows j, j + 16, j + 32 and j + 48 (byte by byte four lanes met in each word).
+            static_assert(XT % kWave == 0 && YT % kWave == 0, "a wavefront brings rows of one operand");
+            const auto pair = __builtin_amdgcn_permlane16_swap(b.v[0], b.v[0], false, false);          // rows of lanes 0 and 2, 1 and 3
+            const auto even = __builtin_amdgcn_permlane32_swap(pair[0], pair[0], false, false), odd = __builtin_amdgcn_permlane32_swap(pair[1], pair[1], false, false);
+            const uint32_t q = (threadIdx.x & 63) >> 4, pick = 0x0c0c0400u + q * 0x0101u;              // byte q of the second, then of the first
+            const uint32_t low = __builtin_amdgcn_perm(odd[0], even[0], pick), high = __builtin_amdgcn_perm(odd[1], even[1], pick);
+            *reinterpret_cast<uint32_t *>(lds + (in_x ? 0 : 4 * XT) + q * rows + (r & 15) * (rows / 16) + (r >> 6) * 4) = low | high << 16;
+            return;
+        }
         uint8_t *const at = lds + (in_x ? 0 : 4 * XT) + (r & 15) * (rows / 16) + (r >> 4);
 #pragma unroll
         for (int h = 0; h < H; ++h)
