@@ -333,7 +333,7 @@ typedef struct dq_classes {
 } dq_classes;
 
 /* Host struct: a teacher's largest logits.  Row t's entries are cls[t*ld + j], logit[t*ld + j], j < k, in any order; a class below 0
- * is an entry that is not there.  A class that comes twice counts twice.  tau > 0: the temperature. */
+ * is an entry that is not there.  A class that comes twice counts twice.  tau > 0: the temperature (finite, and so is 1 / tau). */
 typedef struct dq_teacher {
     int64_t k;
     const int32_t *cls;

@@ -141,3 +141,9 @@ def test_other_arguments_in_four_bits():
     assert lib.dq_mx4_scores_bytes(0, 5) == lib.dq_mx4_row_bytes(0) == lib.dq_mx4_row_scales(-1) == dq.ERR_INVALID_ARG
     assert scores(mx4(d=(1 << 23) + 1, ld_codes=1 << 23, ld_scales=1 << 20), lda=1 << 24) == dq.ERR_UNSUPPORTED
     assert dq.dq_mx4_row_bytes(129) == 128 and dq.dq_mx4_row_scales(129) == 8
+
+
+@pytest.mark.parametrize("tau", [1e-39, 1e-45])
+def test_temperatures_without_an_inverse(tau):
+    assert distill(problem(), teacher(tau=tau)) == dq.ERR_INVALID_ARG
+    assert distill(problem(), teacher(tau=1e-38), nbytes=0) == dq.ERR_WORKSPACE

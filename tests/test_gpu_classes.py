@@ -415,3 +415,33 @@ def test_teacher_over_several_pieces(dq):
     for name, want in (("loss", loss), ("da", p @ w.double()), ("dw", p.mT @ a.double())):
         bound = 1e-5 if name == "loss" else 2 * half_step(torch.bfloat16) + 2e-6
         assert float((got[name].double() - want).norm() / want.norm()) <= bound, name
+
+
+@pytest.mark.parametrize("tau", [0.25, 1.0, 4.0])
+def test_teachers_logits_of_the_lowest_value(dq, tau):
+    """Masked entries are often given the type's lowest number: beside others they have no weight, alone they share the row."""
+    n, c, d, k = 6, 200, 32, 4
+    a, w, g = make(n, c, d, "f32", 31)
+    low = torch.finfo(torch.float32).min
+    cls = torch.stack([torch.randperm(c, generator=g)[:k] for _ in range(n)]).int()
+    logit = torch.randn(n, k, generator=g)
+    logit[0] = low
+    logit[1, 1:] = low
+    logit[2, 2] = low
+    logit[3, :3] = -float("inf")
+    logit[3, 3] = low
+    logit[4] = -float("inf")                                # the only row that is left out
+    u = logit.double() - logit.double().amax(1, keepdim=True)
+    q = torch.softmax(torch.where(torch.isnan(u), 0.0, u) / tau, 1)
+    used = torch.arange(n) != 4
+    full = torch.zeros(n, c, dtype=torch.float64).scatter_add_(1, cls.long(), torch.where(used[:, None], q, 0.0))
+    want = definition(a, w, full, tau, None, 1.0, used)
+    got = run(dq, a.cuda(), w.cuda(), dq.Teacher(cls.cuda(), logit.cuda(), tau), None, 1.0)
+    z = a.double() @ w.double().T / tau
+    spread = z.abs().amax(1) + torch.logsumexp(z, 1).abs() + 1
+    e_q = 2.0 ** -20 * (1 + logit[logit > -100].abs().max().item() / tau)       # as for every teacher
+    f = (tau * used.double())[:, None] * full * e_q
+    extra = dict(loss=tau * tau * e_q * spread, lse=0.0, da=f @ w.double().abs(), dw=f.T @ a.double().abs())
+    for name in want:
+        check(got[name], (want[name][0], want[name][1] + extra[name]), name)
+    assert got["loss"][4] == 0 and not got["da"][4].any() and torch.isfinite(got["loss"]).all()
