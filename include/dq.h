@@ -359,8 +359,8 @@ int32_t dq_class_loss(const dq_classes *prob /*host*/, const int32_t *label, flo
  *   g_tj = scale weight_t (softmax(z_t)_j - [j = label_t]),   da_out = g W  [n][ldda],   dw_out = g^T a  [c][lddw],
  * either nullable, of the problem's type, whole (rows left out: zeros in da_out, nothing to dw_out, whatever the row holds).
  * loss_out, lse_out nullable.  Deterministic: sums in a fixed order.  g itself is rounded to the problem's type (float32: kept
- * whole) for the two products: by at most 2^-8 or 2^-11 of each term; in float16 as a multiple of the largest |weight| that keeps terms
- * down to 2^-29 of it normal.  The outputs must not overlap the inputs. */
+ * whole) for the two products: by at most 2^-8 or 2^-11 of each term; in float16 as a multiple of the largest finite |weight| that keeps
+ * terms down to 2^-28 of it normal.  The outputs must not overlap the inputs. */
 int32_t dq_class_grad(const dq_classes *prob /*host*/, const int32_t *label, const float *weight, float scale,
                       float *loss_out, float *lse_out, void *da_out, int64_t ldda, void *dw_out, int64_t lddw,
                       uint32_t *status, void *ws, int64_t ws_bytes, void *stream);

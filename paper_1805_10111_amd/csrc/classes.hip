@@ -21,7 +21,7 @@ constexpr int kNoClass = 0x7fffffff;
 // Bytes of g.  What is kept of the first piece need not be multiplied again: 8192 rows of 47236 classes (774 MB) in pieces of 512 MB 9.0 ms,
 // in one 8.1; the workspace is a three-hundredth of the card's memory.
 constexpr int64_t kPieceBytes = 1024ll << 20;
-constexpr float kF16Unit = 16384.0f;           // g of float16: terms down to 2^-29 of the largest weight stay normal
+constexpr float kF16Unit = 16384.0f;           // g of float16: terms down to 2^-28 of the largest weight stay normal
 
 // The three bfloat16 whose sum is v.  Infinities and NaNs: the first part alone.
 __device__ __forceinline__ void parts_of(float v, u16 out[3])
@@ -120,8 +120,8 @@ __global__ __launch_bounds__(256) void pack_kernel(Packed a, Packed w, int64_t o
     }
 }
 
-// The largest |weight| of the rows that have a target, for float16, one block.  Held between 2^-100 and the largest finite number: an
-// infinite weight is its own row's matter.
+// The largest finite |weight| of the rows that have a target, for float16, one block.  Held to at least 2^-100.  A weight that is not finite
+// is its own row's matter, whose g is not finite at any unit: taken into the maximum it would make the others' zeros.
 __global__ __launch_bounds__(1024) void weight_max_kernel(const float *__restrict__ weight, int64_t n, Targets targets, float *__restrict__ out)
 {
     __shared__ uint32_t top;
@@ -129,10 +129,13 @@ __global__ __launch_bounds__(1024) void weight_max_kernel(const float *__restric
     __syncthreads();
     uint32_t m = 0;
     for (int64_t t = threadIdx.x; t < n; t += 1024)
-        if (targets.used(t)) m = max(m, __float_as_uint(weight[t]) & 0x7fffffffu);
+        if (targets.used(t)) {
+            const uint32_t w = __float_as_uint(weight[t]) & 0x7fffffffu;
+            if (w < 0x7f800000u) m = max(m, w);
+        }
     atomicMax(&top, m);
     __syncthreads();
-    if (threadIdx.x == 0) out[0] = top ? __uint_as_float(min(max(top, 0x0d800000u), 0x7f7fffffu)) : 1.0f;
+    if (threadIdx.x == 0) out[0] = top ? __uint_as_float(max(top, 0x0d800000u)) : 1.0f;
 }
 
 // One block of 64 threads per row: q = softmax(logit / tau) over the entries, sorted by class (bitonic, in LDS).

@@ -445,3 +445,29 @@ def test_teachers_logits_of_the_lowest_value(dq, tau):
     for name in want:
         check(got[name], (want[name][0], want[name][1] + extra[name]), name)
     assert got["loss"][4] == 0 and not got["da"][4].any() and torch.isfinite(got["loss"]).all()
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("n,c", [(20, 300), (90, 300), (300, 5000)])
+def test_weights_that_are_not_finite_stay_with_their_rows(dq, t, what, n, c):
+    """Of rows that have a target: the gradients of other rows are those of a call in which that weight is an ordinary one."""
+    d = 64
+    a, w, g = make(n, c, d, t, 22)
+    label = torch.randint(0, c, (n,), generator=g, dtype=torch.int32)
+    weight = 0.5 + torch.rand(n, generator=g)
+    weight[7], weight[3] = 2.0, 0.75                        # the largest, and the one that will not be finite
+    clean = run(dq, a.cuda(), w.cuda(), label.cuda(), weight.cuda(), 1.0)
+    weight[3] = what
+    got = run(dq, a.cuda(), w.cuda(), label.cuda(), weight.cuda(), 1.0)
+    others = torch.arange(n) != 3
+    assert torch.equal(got["loss"], clean["loss"]) and torch.equal(got["lse"], clean["lse"])
+    assert torch.equal(got["da"].cpu()[others], clean["da"].cpu()[others]) and clean["da"].cpu()[others].abs().amax(1).min() > 0
+    assert not torch.isfinite(got["da"].cpu()[3]).any() and not torch.isfinite(got["dw"]).any()
+
+
+def test_weights_none_of_which_is_finite(dq):
+    a, w, g = make(30, 300, 64, "f16", 23)
+    label = torch.randint(0, 300, (30,), generator=g, dtype=torch.int32)
+    got = run(dq, a.cuda(), w.cuda(), label.cuda(), torch.full((30,), float("inf"), device="cuda"), 1.0)
+    assert not torch.isfinite(got["da"]).any() and not torch.isfinite(got["dw"]).any() and torch.isfinite(got["loss"]).all()
