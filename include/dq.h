@@ -30,7 +30,7 @@
  *    messages of the worker / master calls use b in {2,4,8} (or 32 = float32, not
  *    quantized); unpacked int8 codes support any b in [2,8].
  *  - `status` (nullable) is a device uint32 that is OR-ed into, never cleared:
- *    bit 0 = a scale delta was not finite (NaN/Inf in the input vector);
+ *    bit 0 = a scale delta was not finite (NaN/Inf in the input vector), or a row's loss;
  *    bit 1 = a class (label, teacher's entry) was not below the number of classes;
  *    bit 31 = dq_run_rounds, where the blocks of one launch do many rounds: they waited for each other
  *    for seconds and gave up, the state is not that of the rounds asked for.  (Without a status word no launch does
@@ -351,7 +351,7 @@ int64_t dq_class_workspace_bytes(int32_t op, const dq_classes *prob /*host*/, in
 
 /* Softmax cross entropy: loss_out[t] = lse_t - z_t,label[t],  lse_t = log sum_j exp z_tj  (lse_out nullable).
  * A row with a label below 0 is left out: its loss is 0 (its lse is still written).  A label of c or more leaves the row out too and
- * sets status bit 1.  Status bit 0: the lse of a row that is not left out is not finite. */
+ * sets status bit 1.  Status bit 0: the lse or the loss of a row that is not left out is not finite. */
 int32_t dq_class_loss(const dq_classes *prob /*host*/, const int32_t *label, float *loss_out, float *lse_out,
                       uint32_t *status, void *ws, int64_t ws_bytes, void *stream);
 
@@ -368,7 +368,7 @@ int32_t dq_class_grad(const dq_classes *prob /*host*/, const int32_t *label, con
 /* Distillation: with q_t = softmax(logit_t / tau) over the entries of row t and p_t = softmax(z_t / tau) over all classes,
  *   loss_out[t] = tau^2 sum_j q_tj (log q_tj - log p_tj),   lse_out[t] = log sum_j exp(z_tj / tau).
  * A row without an entry (or whose logits are all -inf) is left out, as above.  Entries with a class of c or more are not there, and
- * set status bit 1. */
+ * set status bit 1.  An entry whose logit is a NaN or +inf makes its row's loss and gradients NaN (status bit 0). */
 int32_t dq_distill_loss(const dq_classes *prob /*host*/, const dq_teacher *teacher /*host*/, float *loss_out, float *lse_out,
                         uint32_t *status, void *ws, int64_t ws_bytes, void *stream);
 /* The same with gradients:  g_tj = scale weight_t tau (p_tj - q_tj). */

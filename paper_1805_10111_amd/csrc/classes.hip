@@ -380,10 +380,12 @@ struct Finish {
     __device__ __forceinline__ void tell(const Targets &targets, int64_t t, float lse, float hit) const
     {
         const bool live = targets.used(t);
-        if (loss) loss[t] = live ? tau2 * ((entropy ? entropy[t] : 0.0f) + (lse - hit)) : 0.0f;
+        const float value = live ? tau2 * ((entropy ? entropy[t] : 0.0f) + (lse - hit)) : 0.0f;
+        if (loss) loss[t] = value;
         if (lse_out) lse_out[t] = lse;
         const bool far = !targets.q && targets.cls[t] >= static_cast<int64_t>(targets.c);       // (a teacher's were looked at before)
-        const uint32_t said = (live && !__builtin_isfinite(lse) ? 1u : 0u) | (far ? 2u : 0u);
+        // (a teacher's logits that are not finite, and targets with a score of -inf, show in the loss alone)
+        const uint32_t said = (live && !(__builtin_isfinite(lse) && __builtin_isfinite(value)) ? 1u : 0u) | (far ? 2u : 0u);
         if (said && status) atomicOr(status, said);
     }
 };

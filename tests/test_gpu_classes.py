@@ -471,3 +471,39 @@ def test_weights_none_of_which_is_finite(dq):
     label = torch.randint(0, 300, (30,), generator=g, dtype=torch.int32)
     got = run(dq, a.cuda(), w.cuda(), label.cuda(), torch.full((30,), float("inf"), device="cuda"), 1.0)
     assert not torch.isfinite(got["da"]).any() and not torch.isfinite(got["dw"]).any() and torch.isfinite(got["loss"]).all()
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("n,c", [(20, 300), (90, 300), (300, 5000)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+def test_teachers_logits_that_are_not_finite_are_reported(dq, t, n, c, what):
+    """A row's lse is finite whatever its teacher says: the loss is what tells of it."""
+    a, w, g = make(n, c, 64, t, 41)
+    cls, logit = teacher_rows(n, c, 6, g)
+    cls[3] = torch.arange(6, dtype=torch.int32)
+    logit[3] = torch.arange(6)
+    cls[5], logit[5] = -1, what                             # of entries that are not there: nothing
+    clean_status, status, loss_status = (torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(3))
+    clean = run(dq, a.cuda(), w.cuda(), dq.Teacher(cls.cuda(), logit.cuda(), 2.0), None, 1.0, status=clean_status)
+    logit[3, 2] = what
+    T = dq.Teacher(cls.cuda(), logit.cuda(), 2.0)
+    got = run(dq, a.cuda(), w.cuda(), T, None, 1.0, status=status)
+    run(dq, a.cuda(), w.cuda(), T, None, 1.0, grad=False, status=loss_status)
+    others = torch.arange(n) != 3
+    assert clean_status.item() == 0 and status.item() == 1 and loss_status.item() == 1
+    assert torch.isnan(got["loss"].cpu()[3]) and torch.isfinite(got["lse"]).all()
+    assert torch.equal(got["loss"].cpu()[others], clean["loss"].cpu()[others]) and torch.equal(got["da"].cpu()[others], clean["da"].cpu()[others])
+
+
+def test_losses_without_bound_are_reported(dq):
+    """A class whose scores are all -inf: the loss of a row with that label is infinite, its lse is not."""
+    n, c, d = 40, 300, 64
+    a, w, g = make(n, c, d, "bf16", 42)
+    a, label = a.abs() + 0.1, torch.randint(0, c - 1, (n,), generator=g, dtype=torch.int32)
+    w[c - 1] = -float("inf")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = run(dq, a.cuda(), w.cuda(), label.cuda(), None, 1.0, grad=False, status=status)
+    assert status.item() == 0 and torch.isfinite(got["loss"]).all()
+    label[9] = c - 1
+    got = run(dq, a.cuda(), w.cuda(), label.cuda(), None, 1.0, grad=False, status=status)
+    assert status.item() == 1 and got["loss"][9] == float("inf") and torch.isfinite(got["lse"]).all()
