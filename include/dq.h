@@ -346,7 +346,9 @@ typedef struct dq_teacher {
 #define DQ_OP_CLASS_LOSS  4   /* dq_class_loss, dq_distill_loss */
 #define DQ_OP_CLASS_GRAD  5   /* dq_class_grad, dq_distill_grad */
 /* Bytes of workspace of `op`, as dq_workspace_bytes; k: the teacher's, 0 for labels.  The scores of all classes are never kept:
- * the gradients take the classes in pieces whose n columns of gradients fit 1 GB. */
+ * the gradients take the classes in pieces whose n columns of gradients fit 1 GB.  DQ_ERR_UNSUPPORTED, here and in the calls: more than 2^30
+ * classes, 2^20 columns, strides of 2^22 or DQ_MAX_TEACHER entries, and what no launch takes: 2^28 rows (2^26 with a teacher), 2^23 tiles of
+ * 256 x 256 scores (float32: 256 x 128; up to 64 rows: 2^24 tiles of 64 classes). */
 int64_t dq_class_workspace_bytes(int32_t op, const dq_classes *prob /*host*/, int64_t k);
 
 /* Softmax cross entropy: loss_out[t] = lse_t - z_t,label[t],  lse_t = log sum_j exp z_tj  (lse_out nullable).

@@ -430,7 +430,9 @@ __device__ __forceinline__ float row_lse(const Finish &f, int64_t n, int64_t t, 
     return top + logf(rest[0][row].x);
 }
 
-// ROWS rows a block, 256 / ROWS threads a row.
+// ROWS rows a block, 256 / ROWS threads a row: one where there are few rows, else kFinishRows.
+constexpr int kFinishFew = 256, kFinishRows = 16;
+static int64_t finish_blocks(int64_t n) { return n <= kFinishFew ? n : (n + kFinishRows - 1) / kFinishRows; }
 template <int ROWS>
 __global__ __launch_bounds__(256) void finish_kernel(Finish f, int64_t n, Targets targets, float *__restrict__ lse_kept)
 {
@@ -725,7 +727,8 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
     s.td = dims_of(s.tile, parts, false);
     s.tiles_x = (s.c + s.td.x - 1) / s.td.x;
     s.tiles_y = (s.n + s.td.y - 1) / s.td.y;
-    if (s.tiles_x * s.tiles_y > kMost) return DQ_ERR_UNSUPPORTED;
+    if (!launchable(s.tiles_x * s.tiles_y, threads_of(s.tile)) || !launchable(finish_blocks(s.n), 256) || (k && !launchable(s.n, kTeacherThreads)))
+        return DQ_ERR_UNSUPPORTED;
     int64_t at = 0;
     s.cls = room(at, k ? 4 * s.n * s.k : 0);
     s.q = room(at, k ? 4 * s.n * s.k : 0);
@@ -747,12 +750,14 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
         s.ldg = s.piece;
         s.tile_dw = s.n <= 64 && s.c * s.d <= (1 << 20) ? kTileFew : tile_for(s.d, std::min(s.c, s.piece), parts, true, true);
         s.td_dw = dims_of(s.tile_dw, parts, true);
+        if (!launchable(tiles_of(s.d, std::min(s.c, s.piece), s.td_dw), threads_of(s.tile_dw))) return DQ_ERR_UNSUPPORTED;
         // da has few tiles: its classes are split until the chip is full (a block per compute unit, smaller tiles two or more), though not
         // below four steps each.  (Few rows of few classes in 16 bits are not split at all: one launch less, 64 x 1000 x 4096 41 -> 35 us and
         // 16 x 1000 x 256 34 -> 31 us a pass; in float32, whose steps are six products, the same takes 34.5 -> 38 us.)
         s.tile_da = s.n <= 16 ? kTileFewest : s.n <= 64 ? kTileFew : s.n * s.d <= 256 * 1024 ? kTileMiddle : kTileLarge;
         s.td_da = dims_of(s.tile_da, parts, true);
         const int64_t tiles = tiles_of(s.d, s.n, s.td_da), blocks = s.tile_da == kTileLarge ? 256 : 512;
+        if (!launchable(tiles, threads_of(s.tile_da))) return DQ_ERR_UNSUPPORTED;
         const int64_t most_splits = !parts && s.n <= 64 && s.piece <= 1024 ? 1 : std::clamp<int64_t>(s.piece / 128, 1, std::max<int64_t>(blocks / tiles, 1));
         s.splits = 1;
         double best = 1e30;
@@ -855,8 +860,9 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     const Finish finish{sums, hits, tiles_x, entropy, tau * tau, q.loss, q.lse, q.status};
     const bool finish_later = products && s.pieces == 1 && n <= 256 && c <= 4096;      // (by the gradients' first kernel)
     if (!finish_later) {
-        if (n <= 256) finish_kernel<1><<<static_cast<unsigned>(n), 256, 0, st>>>(finish, n, targets, q.grad ? lse : nullptr);
-        else finish_kernel<16><<<static_cast<unsigned>((n + 15) / 16), 256, 0, st>>>(finish, n, targets, q.grad ? lse : nullptr);
+        const unsigned blocks = static_cast<unsigned>(finish_blocks(n));
+        if (n <= kFinishFew) finish_kernel<1><<<blocks, 256, 0, st>>>(finish, n, targets, q.grad ? lse : nullptr);
+        else finish_kernel<kFinishRows><<<blocks, 256, 0, st>>>(finish, n, targets, q.grad ? lse : nullptr);
         DQ_LAUNCH_CHECK();
     }
     if (!products) return DQ_OK;

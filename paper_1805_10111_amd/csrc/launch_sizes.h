@@ -10,6 +10,8 @@ namespace dq {
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t packed_words(int64_t d, int b) { return (d * b + 31) / 32; }
 inline int64_t pad4(int64_t d) { return (d + 3) / 4 * 4; }
+// A dimension of a launch has fewer than 2^32 threads.
+inline bool launchable(int64_t blocks, int threads) { return blocks <= 0xffffffffll / threads; }
 
 // ------------------------------------------------------------------ full gradient on dense features (grad_dense.hip)
 // Threads per block and float4 columns per thread on rows of more than 1024 floats: of 256 to 512 threads in whole

@@ -668,6 +668,7 @@ constexpr TileDims dims_of(TileSize s, bool parts, bool across)
            s == kTileFew ? TileDims{64, 64} : TileDims{across ? 128 : 64, 16};
 }
 inline int64_t tiles_of(int64_t x, int64_t y, TileDims t) { return (x + t.x - 1) / t.x * ((y + t.y - 1) / t.y); }
+constexpr int threads_of(TileSize s) { return s == kTileLarge ? 512 : 256; }
 
 // The tile that is through first, of large ones (one block to a compute unit, 256 of which take 1), half ones and middle ones (two; where 256
 // or fewer are left over, each has a compute unit to itself and takes 0.6 as long).  Measured on large products in bfloat16: 512 half ones take
@@ -691,11 +692,11 @@ inline TileSize tile_for_rows(int64_t x, int64_t rows, bool parts, bool half)
 // kernels of half tiles and of the smallest.
 #define DQ_TILE_CASE(kernel, what, parts, size, half, few, launch, ...)                                                        \
     switch (size) {                                                                                                            \
-    case kTileLarge: kernel<what, 256, parts ? 128 : 256, 2, 4, 1, parts ? 2 : 4, parts ? 3 : 1><<<launch(512)>>>(__VA_ARGS__); break;     \
-    case kTileHalf: half<<<launch(256)>>>(__VA_ARGS__); break;                                                                 \
-    case kTileMiddle: kernel<what, 128, parts ? 64 : 128, 2, 2, 1, parts ? 2 : 4, parts ? 3 : 1><<<launch(256)>>>(__VA_ARGS__); break;     \
-    case kTileFew: kernel<what, 64, 64, 2, 2, parts ? 1 : 2, 4, parts ? 3 : 1><<<launch(256)>>>(__VA_ARGS__); break;          \
-    case kTileFewest: few<<<launch(256)>>>(__VA_ARGS__); break;                                                                \
+    case kTileLarge: kernel<what, 256, parts ? 128 : 256, 2, 4, 1, parts ? 2 : 4, parts ? 3 : 1><<<launch(threads_of(kTileLarge))>>>(__VA_ARGS__); break;     \
+    case kTileHalf: half<<<launch(threads_of(kTileHalf))>>>(__VA_ARGS__); break;                                                                 \
+    case kTileMiddle: kernel<what, 128, parts ? 64 : 128, 2, 2, 1, parts ? 2 : 4, parts ? 3 : 1><<<launch(threads_of(kTileMiddle))>>>(__VA_ARGS__); break;     \
+    case kTileFew: kernel<what, 64, 64, 2, 2, parts ? 1 : 2, 4, parts ? 3 : 1><<<launch(threads_of(kTileFew))>>>(__VA_ARGS__); break;          \
+    case kTileFewest: few<<<launch(threads_of(kTileFewest))>>>(__VA_ARGS__); break;                                                                \
     }
 
 }  // namespace dq

@@ -218,13 +218,18 @@ static int32_t dequantize4(const dq_mx4 &q, void *out, int64_t ld, hipStream_t s
     return DQ_OK;
 }
 
+// Whether a launch takes the product of n rows with c.
+static bool product_fits(int64_t n, int64_t c)
+{
+    const TileSize size = tile_for_rows(c, n, false, false);
+    return launchable(tiles_of(c, n, dims_of(size, false, false)), threads_of(size));
+}
 template <int TYPE>
 static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int64_t ld, hipStream_t st)
 {
     const TileSize size = tile_for_rows(w.n, a.n, false, false);
     const TileDims t = dims_of(size, false, false);
     const int64_t tiles_x = (w.n + t.x - 1) / t.x, tiles_y = (a.n + t.y - 1) / t.y;
-    if (tiles_x * tiles_y > kMost4) return DQ_ERR_UNSUPPORTED;
     auto operand = [](const dq_mx4 &q) { return Operand{reinterpret_cast<const char *>(q.codes), q.ld_codes, q.n, static_cast<int32_t>(groups_of(q.d) * 32), 0, q.scales, q.ld_scales}; };
 #define DQ_GRID(threads) static_cast<unsigned>(tiles_x * tiles_y), threads, 0, st
     DQ_TILE_CASE(mx4_product_kernel, TYPE, false, size, (mx4_product_kernel<TYPE, 128, 128, 2, 2, 1, 4, 1>), (mx4_product_kernel<TYPE, 64, 16, 4, 1, 2, 4, 1>), DQ_GRID, operand(w), operand(a), groups_of(a.d) * 32,
@@ -272,6 +277,7 @@ extern "C" int32_t dq_mx4_product(const dq_mx4 *a, const dq_mx4 *w, void *out, i
     if (const int32_t e = dq::check4(w)) return e;
     if (a->d != w->d) return DQ_ERR_INVALID_ARG;
     if (const int32_t e = dq::check_matrix(out, type, w->n, ld)) return e;
+    if (!dq::product_fits(a->n, w->n)) return DQ_ERR_UNSUPPORTED;
     return dq::product4(*a, *w, out, type, ld, static_cast<hipStream_t>(stream));
 }
 
@@ -287,7 +293,7 @@ extern "C" int32_t dq_mx4_scores(const void *a, int32_t type, int64_t n, int64_t
 {
     if (const int32_t e = dq::check4(w)) return e;
     if (n <= 0) return DQ_ERR_INVALID_ARG;
-    if (n > dq::kMost4) return DQ_ERR_UNSUPPORTED;
+    if (n > dq::kMost4 || !dq::product_fits(n, w->n)) return DQ_ERR_UNSUPPORTED;
     if (const int32_t e = dq::check_matrix(a, type, w->d, lda)) return e;
     if (const int32_t e = dq::check_matrix(out, out_type, w->n, ld)) return e;
     if (!ws || !dq::aligned16(ws)) return DQ_ERR_INVALID_ARG;

@@ -147,3 +147,34 @@ def test_other_arguments_in_four_bits():
 def test_temperatures_without_an_inverse(tau):
     assert distill(problem(), teacher(tau=tau)) == dq.ERR_INVALID_ARG
     assert distill(problem(), teacher(tau=1e-38), nbytes=0) == dq.ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("bad", [dict(n=1 << 20, c=1 << 19, d=8), dict(n=1 << 20, c=1 << 20, d=8), dict(n=1, c=1 << 30, d=8), dict(n=20, c=1 << 30, d=8),
+                                 dict(n=1 << 28, c=2, d=8), dict(n=1 << 30, c=1 << 30, d=8)], ids=str)
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+def test_problems_that_no_launch_takes(t, bad):
+    """A launch has fewer than 2^32 threads: 2^23 tiles of 512, 2^24 of 256, 2^28 rows of 16."""
+    p = problem(t, **bad)
+    assert size(p, dq.OP_CLASS_LOSS) == size(p, dq.OP_CLASS_GRAD) == loss(p) == grad(p) == dq.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("good", [dict(n=1 << 20, c=(1 << 19) - 256, d=8), dict(n=1, c=(1 << 30) - 64, d=8), dict(n=20, c=(1 << 30) - 64, d=8),
+                                  dict(n=(1 << 28) - 16, c=2, d=8)], ids=str)
+def test_the_largest_problems_that_a_launch_takes(good):
+    p = problem(BF16, **good)
+    assert size(p, dq.OP_CLASS_LOSS) > 0 and size(p) > 0 and loss(p, nbytes=0) == dq.ERR_WORKSPACE
+
+
+def test_teachers_of_more_rows_than_a_launch_takes():
+    """One block of 64 threads a row: 2^26 rows."""
+    few, many = problem(n=(1 << 26) - 1, c=2, d=8), problem(n=1 << 26, c=2, d=8)
+    assert size(few, k=4) > 0 and distill(few, teacher(), nbytes=0) == dq.ERR_WORKSPACE
+    assert size(many, k=4) == distill(many, teacher()) == dq.ERR_UNSUPPORTED and size(many) > 0
+
+
+@pytest.mark.parametrize("n", [1, 16, 17, 64])
+def test_products_in_four_bits_that_no_launch_takes(n):
+    """2^24 tiles of 64 classes; refused before the rows are quantized."""
+    w, a = mx4(n=1 << 30, d=128, ld_codes=64, ld_scales=4), mx4(n=n, d=128, ld_codes=64, ld_scales=4)
+    assert api._lib.dq_mx4_product(C.byref(a), C.byref(w), AT, BF16, 1 << 30, None) == dq.ERR_UNSUPPORTED
+    assert scores(w, n=n, ld=1 << 30) == dq.ERR_UNSUPPORTED
