@@ -315,10 +315,10 @@ int32_t dq_acc_snapshot(const float *xsum, int64_t m, int64_t d, float *x_snap_o
 /* ---- models of many classes ------------------------------------------------------- */
 
 /* The binary model of eq. (1) taken to c classes: a row a_t of features has the scores z_t = W a_t, W [c][d].
- * Types of the features and of the model (one for both, and for their gradients): float32, float16, bfloat16.  Sums, scores,
- * probabilities and losses are float32 throughout; products of float32 are carried out to float32's own precision on the matrix
- * cores, in three bfloat16 parts (magnitudes of 2^127 * 1.99 and more count as infinite; anything not finite gives losses that
- * are not finite). */
+ * Types of the features and of the model (one for both, and for their gradients): float32, float16, bfloat16.  Sums, scores, their
+ * maxima and sums of exponentials, and losses are float32 (what 16-bit gradients are made from: at dq_class_grad); products of
+ * float32 are carried out to float32's own precision on the matrix cores, in three bfloat16 parts (magnitudes of 2^127 * 1.99 and
+ * more count as infinite; anything not finite gives losses that are not finite). */
 #define DQ_F32   0
 #define DQ_F16   1
 #define DQ_BF16  2
@@ -360,9 +360,12 @@ int32_t dq_class_loss(const dq_classes *prob /*host*/, const int32_t *label, flo
 /* The same losses, and the gradients of  scale * sum_t weight[t] loss_t  (weight nullable: all 1):
  *   g_tj = scale weight_t (softmax(z_t)_j - [j = label_t]),   da_out = g W  [n][ldda],   dw_out = g^T a  [c][lddw],
  * either nullable, of the problem's type, whole (rows left out: zeros in da_out, nothing to dw_out, whatever the row holds).
- * loss_out, lse_out nullable.  Deterministic: sums in a fixed order.  g itself is rounded to the problem's type (float32: kept
- * whole) for the two products: by at most 2^-8 or 2^-11 of each term; in float16 as a multiple of the largest finite |weight| that keeps
- * terms down to 2^-28 of it normal.  The outputs must not overlap the inputs. */
+ * loss_out, lse_out nullable.  Deterministic: sums in a fixed order.  The outputs must not overlap the inputs.
+ * g is rounded to the problem's type for the two products (float32: kept whole), by up to 2^-8 of each term in bfloat16 and 2^-11 in
+ * float16, there as a multiple of the largest finite |weight| that keeps terms down to 2^-28 of it normal.  Before that, in 16-bit calls of more
+ * than 64 rows, softmax(z_t)_j of classes without a target is off by a factor of up to 1 -+ 0.00071 in bfloat16 and 0.00018 in float16 (kept as a
+ * 16-bit logarithm; classes behind the first piece: not), and zero below 2^-128 (float16 2^-32) of the largest among its tile's, 128 or 256
+ * neighbouring classes. */
 int32_t dq_class_grad(const dq_classes *prob /*host*/, const int32_t *label, const float *weight, float scale,
                       float *loss_out, float *lse_out, void *da_out, int64_t ldda, void *dw_out, int64_t lddw,
                       uint32_t *status, void *ws, int64_t ws_bytes, void *stream);

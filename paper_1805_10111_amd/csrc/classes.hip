@@ -214,8 +214,9 @@ constexpr int kEdge = 4;               // with a type: rows that are read in pla
 
 // The scores of the first piece stay in the place of its gradients, 16 bits of them in each plane: as they are, in two halves, in float32
 // and where there are few rows; else how far they lie below the tile's maximum, in 65535 steps up to a factor of 2^-128 (2^-32 in
-// float16), behind which probabilities are zeros.  That is off by half a step, a factor of 1 -+ 0.0007 (0.00017): a fifth (a third) of
-// what g's own rounding may be.  The targets' scores, where p - q may cancel, are kept whole.
+// float16), behind which probabilities are zeros.  That is off by half a step, a factor of up to 1 -+ 0.00071 (0.00018, with the conversion's own
+// rounding).  With g's rounding, which is up to 0.0039 (0.00049) of a term, terms came out up to 0.0046 (0.00066) off and in root mean squares
+// 0.00171 instead of 0.00166 (0.00023 and 0.00021).  The targets' scores, where p - q may cancel, are kept whole.
 struct Kept {
     u16 *g;                            // null: none
     int64_t ldg, plane, cols;          // numbers; classes of the piece

@@ -507,3 +507,36 @@ def test_losses_without_bound_are_reported(dq):
     label[9] = c - 1
     got = run(dq, a.cuda(), w.cuda(), label.cuda(), None, 1.0, grad=False, status=status)
     assert status.item() == 1 and got["loss"][9] == float("inf") and torch.isfinite(got["lse"]).all()
+
+
+@pytest.mark.parametrize("t,scale", [("bf16", 1.0), ("f16", 1.0), ("f16", 1024.0)])
+@pytest.mark.parametrize("n,c,spread", [(64, 900, 3.0), (65, 900, 3.0), (128, 3000, 1.0), (200, 30000, 3.0), (520, 20011, 2.0), (1000, 40000, 6.0)])
+def test_each_term_of_g(dq, t, scale, n, c, spread):
+    """Features that are the unit vectors: z_tj = w_jt and dw_jt = g_tj, one term each, with no sums between it and its roundings.
+    With R = 128 (float16 32): probabilities of up to 64 rows are float32's, of more kept as logarithms of base 2 below their tile's maximum,
+    in steps of R / 65535 (half a step, and 0.01 for the conversion's own arithmetic), and zeros from R on; R 2^-22 and 2^-18 are the roundings of
+    those logarithms and the exponential's.  Then g's rounding: half a step, in float16 at least that of 2^-14 2^-14 (the unit is 2^14);
+    and the output's, of float16's smallest numbers too.  Targets' own scores are whole."""
+    w = (torch.randn(c, n, generator=torch.Generator().manual_seed(c)) * spread).to(TYPES[t])
+    label = torch.randint(0, c, (n,), generator=torch.Generator().manual_seed(n), dtype=torch.int32)
+    w[label[::3].long(), torch.arange(n)[::3]] += 2 * spread           # a third of the rows are nearly right
+    a, w, label = torch.eye(n, dtype=TYPES[t], device="cuda"), w.cuda(), label.cuda()
+    got = run(dq, a, w, label, None, scale, da=False)["dw"].double().T
+    z = w.double().T.contiguous()
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    p = torch.exp(z - lse)
+    g = p.clone()
+    at = (torch.arange(n, device="cuda"), label.long())
+    g[at] -= 1.0
+    r = 128.0 if t == "bf16" else 32.0
+    own = 2.0 ** -21 * (1 + z.abs() + lse.abs()) + 2.0 ** -20
+    kept = own if n <= 64 else own + (2.0 ** (0.51 * r / 65535) - 1 + r * 2.0 ** -22 + 2.0 ** -18)
+    off = p * kept
+    if n > 64:
+        off = torch.where(p <= 2.0 ** -(r - 0.001) * p.amax(1, keepdim=True), p, off)
+    off[at] = (p * own)[at]
+    off = (off + half_step(TYPES[t]) * (g.abs() + off) + (2.0 ** -39 if t == "f16" else 0.0)) * scale
+    if t == "f16":
+        off = off + half_step(torch.float16) * (scale * g.abs() + off) + 2.0 ** -25
+    worst = ((got - scale * g).abs() / (off + 1e-300)).max().item()
+    assert worst <= 1.0, worst
