@@ -18,9 +18,6 @@
 namespace dq {
 
 constexpr int kNoClass = 0x7fffffff;
-// Bytes of g.  What is kept of the first piece need not be multiplied again: 8192 rows of 47236 classes (774 MB) in pieces of 512 MB 9.0 ms,
-// in one 8.1; the workspace is a three-hundredth of the card's memory.
-constexpr int64_t kPieceBytes = 1024ll << 20;
 constexpr float kF16Unit = 16384.0f;           // g of float16: terms down to 2^-28 of the largest weight stay normal
 
 // The three bfloat16 whose sum is v.  Infinities and NaNs: the first part alone.
@@ -222,7 +219,6 @@ struct Kept {
     int64_t ldg, plane, cols;          // numbers; classes of the piece
     float *target_z;                   // z of the targets' entries, null in calls without gradients
 };
-constexpr bool kept_whole(int type, int x) { return type == DQ_F32 || x <= 64; }
 template <int TYPE>
 struct KeptUnit {
     static constexpr float kRange = TYPE == DQ_F16 ? 32.0f : 128.0f;
@@ -264,7 +260,7 @@ __global__ __launch_bounds__(WX *WY *kWave, 2) void scores_kernel(Operand w, Ope
         }
     });
     // Where what is kept is relative, scores are taken in units of a factor of two, which saves a product each.
-    constexpr bool kBits = !kept_whole(TYPE, XT);
+    constexpr bool kBits = !kept_whole(TYPE == DQ_F32, XT);
     const float unit = kBits ? kLn2 : 1.0f, per_unit = kBits ? inv_tau * kLog2E : inv_tau;
     auto exp_of = [](float v) { return kBits ? __builtin_amdgcn_exp2f(v) : TYPE == DQ_F32 ? expf(v) : exp_near(v); };
     const int lane = threadIdx.x & 63, base = static_cast<int>(c0) + Tile::at_x(0);
@@ -347,7 +343,7 @@ __global__ __launch_bounds__(WX *WY *kWave, 2) void scores_kernel(Operand w, Ope
     }
     if (!kept.g || c0 >= kept.cols) return;
     u16 *const to = kept.g + t0 * kept.ldg + c0;
-    if constexpr (kept_whole(TYPE, XT)) {
+    if constexpr (kept_whole(TYPE == DQ_F32, XT)) {
 #pragma unroll
         for (int p = 0; p < 2; ++p)
             tile.store(to + p * kept.plane, kept.ldg, YT, XT, [&](int m, int y) {
@@ -464,7 +460,7 @@ __global__ __launch_bounds__(256) void kept_kernel(Kept kept, int64_t cols, int6
                                                    const float *__restrict__ weight_max)
 {
     typedef __attribute__((ext_vector_type(8))) u16 Eight;
-    constexpr bool kWhole = kept_whole(TYPE, XT);
+    constexpr bool kWhole = kept_whole(TYPE == DQ_F32, XT);
     constexpr int kPlanes = TYPE == DQ_F32 ? 3 : 1;
     const int64_t first = blockIdx.x * 2048ll, i = first + threadIdx.x * 8;
     for (int64_t t = blockIdx.y; t < rows; t += gridDim.y) {
@@ -743,34 +739,18 @@ static int32_t class_plan(const dq_classes *p, int64_t k, bool grad, ClassPlan &
     if (grad) {
         s.rows_z = up(s.n, 32);
         s.rows_g = s.tiles_y * s.td.y;
-        s.planes_g = std::max(s.planes, kept_whole(s.type, s.td.x) ? 2 : 1);
-        const int64_t most = std::max<int64_t>(kPieceBytes / (2 * s.planes_g * s.rows_g) / 256, 1) * 256;
-        s.pieces = (s.c + most - 1) / most;
-        s.piece = s.pieces > 1 ? most : up(s.c, 256);          // (the first one's scores are kept: it takes all that there is room for)
-        s.pieces = (s.c + s.piece - 1) / s.piece;
+        s.planes_g = planes_of_g(parts, s.td.x);
+        s.piece = piece_of(s.c, s.rows_g, s.planes_g);
+        s.pieces = ceil_div(s.c, s.piece);
         s.ldg = s.piece;
-        s.tile_dw = s.n <= 64 && s.c * s.d <= (1 << 20) ? kTileFew : tile_for(s.d, std::min(s.c, s.piece), parts, true, true);
+        s.tile_dw = tile_for_dw(s.n, s.c, s.d, s.piece, parts);
         s.td_dw = dims_of(s.tile_dw, parts, true);
-        if (!launchable(tiles_of(s.d, std::min(s.c, s.piece), s.td_dw), threads_of(s.tile_dw))) return DQ_ERR_UNSUPPORTED;
-        // da has few tiles: its classes are split until the chip is full (a block per compute unit, smaller tiles two or more), though not
-        // below four steps each.  (Few rows of few classes in 16 bits are not split at all: one launch less, 64 x 1000 x 4096 41 -> 35 us and
-        // 16 x 1000 x 256 34 -> 31 us a pass; in float32, whose steps are six products, the same takes 34.5 -> 38 us.)
-        s.tile_da = s.n <= 16 ? kTileFewest : s.n <= 64 ? kTileFew : s.n * s.d <= 256 * 1024 ? kTileMiddle : kTileLarge;
+        s.tile_da = tile_for_da(s.n, s.d);
         s.td_da = dims_of(s.tile_da, parts, true);
-        const int64_t tiles = tiles_of(s.d, s.n, s.td_da), blocks = s.tile_da == kTileLarge ? 256 : 512;
-        if (!launchable(tiles, threads_of(s.tile_da))) return DQ_ERR_UNSUPPORTED;
-        const int64_t most_splits = !parts && s.n <= 64 && s.piece <= 1024 ? 1 : std::clamp<int64_t>(s.piece / 128, 1, std::max<int64_t>(blocks / tiles, 1));
-        s.splits = 1;
-        double best = 1e30;
-        for (int64_t i = 1; i <= most_splits; ++i) {         // fewest rounds for the work of one split, and something for its sums
-            const double cost = static_cast<double>((tiles * i + blocks - 1) / blocks) / static_cast<double>(i) * (1.0 + 0.01 * static_cast<double>(i));
-            if (cost < best) {
-                best = cost;
-                s.splits = i;
-            }
-        }
-        s.per_split = up((s.piece + s.splits - 1) / s.splits, 32);
-        s.splits = (s.piece + s.per_split - 1) / s.per_split;
+        if (!launchable(tiles_of(s.d, std::min(s.c, s.piece), s.td_dw), threads_of(s.tile_dw)) || !launchable(tiles_of(s.d, s.n, s.td_da), threads_of(s.tile_da)))
+            return DQ_ERR_UNSUPPORTED;
+        s.per_split = da_split(s.n, s.d, s.piece, parts);
+        s.splits = ceil_div(s.piece, s.per_split);
         s.da_at_once = s.splits == 1 && s.pieces == 1;
         s.az = room(at, 2 * s.planes * s.rows_z * s.dp);
         s.target_z = room(at, 4 * s.n * s.k);

@@ -229,4 +229,80 @@ inline bool csr_rounds_shape(int64_t d, int64_t n, int64_t entries, int64_t M, i
     return true;
 }
 
+// ------------------------------------------------------------------ products of many-class models (matrix_tile.h, classes.hip, mx4.hip)
+// Tiles of the products, and how many of their blocks a compute unit has at a time.
+enum TileSize { kTileLarge, kTileHalf, kTileMiddle, kTileFew, kTileFewest };
+struct TileDims {
+    int x, y;
+};
+// x by y results a tile.  float32 in parts takes three times the room in LDS, and tiles half as high (and no half ones).  The last: 64 by
+// 16 rows, of 128 columns where x is stored across k.
+constexpr TileDims dims_of(TileSize s, bool parts, bool across)
+{
+    return s == kTileLarge ? TileDims{256, parts ? 128 : 256} : s == kTileHalf ? TileDims{256, 128} : s == kTileMiddle ? TileDims{128, parts ? 64 : 128} :
+           s == kTileFew ? TileDims{64, 64} : TileDims{across ? 128 : 64, 16};
+}
+inline int64_t tiles_of(int64_t x, int64_t y, TileDims t) { return (x + t.x - 1) / t.x * ((y + t.y - 1) / t.y); }
+constexpr int threads_of(TileSize s) { return s == kTileLarge ? 512 : 256; }
+
+// The tile that is through first, of large ones (one block to a compute unit, 256 of which take 1), half ones and middle ones (two; where 256
+// or fewer are left over, each has a compute unit to itself and takes 0.6 as long).  Measured on large products in bfloat16: 512 half ones take
+// 1.1 (operands along k: 8192 x 47236 x 4096 in 2.81 and 3.10 ms), both operands across k 0.93 (47236 x 4096 x 8192 in 2.46 and 2.29 ms),
+// 512 middle ones 0.7 for their half of the work.
+inline TileSize tile_for(int64_t x, int64_t y, bool parts, bool half, bool across)
+{
+    auto pairs = [](int64_t tiles, double each) { return each * (static_cast<double>(tiles / 512) + (tiles % 512 > 256 ? 1.0 : tiles % 512 ? 0.6 : 0.0)); };
+    const double large = static_cast<double>((tiles_of(x, y, dims_of(kTileLarge, parts, across)) + 255) / 256);
+    const double halves = half && !parts ? pairs(tiles_of(x, y, dims_of(kTileHalf, parts, across)), across ? 0.93 : 1.1) : large;
+    const double middle = pairs(tiles_of(x, y, dims_of(kTileMiddle, parts, across)), 0.7);
+    return middle < large && middle < halves ? kTileMiddle : halves < large ? kTileHalf : kTileLarge;
+}
+// ... of products over `rows` rows.
+inline TileSize tile_for_rows(int64_t x, int64_t rows, bool parts, bool half)
+{
+    return rows <= 16 ? kTileFewest : rows <= 64 ? kTileFew : tile_for(x, rows, parts, half, false);
+}
+// ... of dW, c classes (a piece at a time) of d columns.  Few rows of few classes: small tiles, of which there are more.
+inline TileSize tile_for_dw(int64_t n, int64_t c, int64_t d, int64_t piece, bool parts)
+{
+    return n <= 64 && c * d <= (1 << 20) ? kTileFew : tile_for(d, c < piece ? c : piece, parts, true, true);
+}
+// ... of da, n rows of d columns.
+inline TileSize tile_for_da(int64_t n, int64_t d) { return n <= 16 ? kTileFewest : n <= 64 ? kTileFew : n * d <= 256 * 1024 ? kTileMiddle : kTileLarge; }
+
+// Whether 32 bits of each score are kept for the gradients, in tiles of x classes (up to 64 rows), and 16-bit planes of scores or gradients.
+constexpr bool kept_whole(bool parts, int x) { return parts || x <= 64; }
+constexpr int planes_of_g(bool parts, int x) { return parts ? 3 : kept_whole(parts, x) ? 2 : 1; }
+
+// Bytes of g.  What is kept of the first piece need not be multiplied again: 8192 rows of 47236 classes (774 MB) in pieces of 512 MB 9.0 ms,
+// in one 8.1; the workspace is a three-hundredth of the card's memory.
+constexpr int64_t kPieceBytes = 1024ll << 20;
+// Classes of a piece of c: all (in whole tiles), or as many as there is room for, as the first one's scores are kept.
+inline int64_t piece_of(int64_t c, int64_t rows, int planes)
+{
+    const int64_t room = kPieceBytes / (2 * planes * rows) / 256, most = (room > 1 ? room : 1) * 256;
+    return c > most ? most : ceil_div(c, 256) * 256;
+}
+
+// Classes of one split of da's piece.  da has few tiles: its classes are split until the chip is full (a block per compute unit, smaller
+// tiles two or more), though not below four steps each.  (Few rows of few classes in 16 bits are not split at all: one launch less, 64 x 1000 x
+// 4096 41 -> 35 us and 16 x 1000 x 256 34 -> 31 us a pass; in float32, whose steps are six products, the same takes 34.5 -> 38 us.)
+inline int64_t da_split(int64_t n, int64_t d, int64_t piece, bool parts)
+{
+    const TileSize tile = tile_for_da(n, d);
+    const int64_t tiles = tiles_of(d, n, dims_of(tile, parts, true)), blocks = tile == kTileLarge ? 256 : 512;
+    const auto between = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
+    const int64_t most = !parts && n <= 64 && piece <= 1024 ? 1 : between(piece / 128, 1, between(blocks / tiles, 1, blocks));
+    int64_t splits = 1;
+    double best = 1e30;
+    for (int64_t i = 1; i <= most; ++i) {                // fewest rounds for the work of one split, and something for its sums
+        const double cost = static_cast<double>((tiles * i + blocks - 1) / blocks) / static_cast<double>(i) * (1.0 + 0.01 * static_cast<double>(i));
+        if (cost < best) {
+            best = cost;
+            splits = i;
+        }
+    }
+    return ceil_div(ceil_div(piece, splits), 32) * 32;
+}
+
 }  // namespace dq

@@ -21,6 +21,7 @@
 #include <hip/hip_fp16.h>
 
 #include "dq_common.h"
+#include "launch_sizes.h"
 
 namespace dq {
 
@@ -643,6 +644,7 @@ __device__ __forceinline__ void store_four(typename Num<TYPE>::Mem *to, f32x4 v,
 // vector stores of four results where every row allows them
 static bool four_at_once(const void *p, int64_t ld, int wide) { return reinterpret_cast<uintptr_t>(p) % (4 * wide) == 0 && ld % 4 == 0; }
 
+// (Which sizes of tiles there are and the rules that choose them: launch_sizes.h.)
 // Which tile a block takes: the blocks of a die (every eighth) take neighbouring tiles, in groups of kGroup rows of y tiles, so that
 // those at work at one time share both operands in the die's 4 MB of L2.
 __device__ __forceinline__ void tile_of_block(int block, int tiles_x, int tiles_y, int &tx, int &ty)
@@ -653,39 +655,6 @@ __device__ __forceinline__ void tile_of_block(int block, int tiles_x, int tiles_
     const int span = kGroup * tiles_x, group = t / span, first = group * kGroup, high = min(kGroup, tiles_y - first), in = t % span;
     ty = first + in % high;
     tx = in / high;
-}
-
-// Tiles of the products, and how many of their blocks a compute unit has at a time.
-enum TileSize { kTileLarge, kTileHalf, kTileMiddle, kTileFew, kTileFewest };
-struct TileDims {
-    int x, y;
-};
-// x by y results a tile.  float32 in parts takes three times the room in LDS, and tiles half as high (and no half ones).  The last: 64 by
-// 16 rows, of 128 columns where x is stored across k.
-constexpr TileDims dims_of(TileSize s, bool parts, bool across)
-{
-    return s == kTileLarge ? TileDims{256, parts ? 128 : 256} : s == kTileHalf ? TileDims{256, 128} : s == kTileMiddle ? TileDims{128, parts ? 64 : 128} :
-           s == kTileFew ? TileDims{64, 64} : TileDims{across ? 128 : 64, 16};
-}
-inline int64_t tiles_of(int64_t x, int64_t y, TileDims t) { return (x + t.x - 1) / t.x * ((y + t.y - 1) / t.y); }
-constexpr int threads_of(TileSize s) { return s == kTileLarge ? 512 : 256; }
-
-// The tile that is through first, of large ones (one block to a compute unit, 256 of which take 1), half ones and middle ones (two; where 256
-// or fewer are left over, each has a compute unit to itself and takes 0.6 as long).  Measured on large products in bfloat16: 512 half ones take
-// 1.1 (operands along k: 8192 x 47236 x 4096 in 2.81 and 3.10 ms), both operands across k 0.93 (47236 x 4096 x 8192 in 2.46 and 2.29 ms),
-// 512 middle ones 0.7 for their half of the work.
-inline TileSize tile_for(int64_t x, int64_t y, bool parts, bool half, bool across)
-{
-    auto pairs = [](int64_t tiles, double each) { return each * (static_cast<double>(tiles / 512) + (tiles % 512 > 256 ? 1.0 : tiles % 512 ? 0.6 : 0.0)); };
-    const double large = static_cast<double>((tiles_of(x, y, dims_of(kTileLarge, parts, across)) + 255) / 256);
-    const double halves = half && !parts ? pairs(tiles_of(x, y, dims_of(kTileHalf, parts, across)), across ? 0.93 : 1.1) : large;
-    const double middle = pairs(tiles_of(x, y, dims_of(kTileMiddle, parts, across)), 0.7);
-    return middle < large && middle < halves ? kTileMiddle : halves < large ? kTileHalf : kTileLarge;
-}
-// ... of products over `rows` rows.
-inline TileSize tile_for_rows(int64_t x, int64_t rows, bool parts, bool half)
-{
-    return rows <= 16 ? kTileFewest : rows <= 64 ? kTileFew : tile_for(x, rows, parts, half, false);
 }
 
 // kernel<what, x, y, WX, WY, H, R, P> in a tile's size: its wavefronts, steps a stage, stages in the ring, parts of a number.  half, few: the

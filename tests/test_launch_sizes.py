@@ -159,3 +159,28 @@ def test_launches_with_equal_parts_of_all_dies_pick_different_ones(tmp_path):
         if (times[i] != (i < 8 ? 100 : 0)) std::printf("die %u: %d\\n", i, times[i]);
     """)
     assert out == "", out[:2000]
+
+
+def test_pieces_and_splits_of_many_classes(tmp_path):
+    """Rows and classes of every size: pieces are whole tiles of classes and fit their room, the splits of a piece are whole steps that
+    cover it, no more of them than fill the chip."""
+    out = _sweep(tmp_path, """
+    for (int64_t n = 1; n < (1ll << 28); n += 1 + n / 7)
+        for (int64_t c = 1; c < (1ll << 30); c += 1 + c / 5)
+            for (int parts = 0; parts < 2; ++parts) {
+                const TileSize s = tile_for_rows(c, n, parts, true);
+                const TileDims t = dims_of(s, parts, false);
+                const int64_t rows = ceil_div(n, t.y) * t.y;
+                const int planes = planes_of_g(parts, t.x);
+                const int64_t piece = piece_of(c, rows, planes);
+                if (piece % 256 || piece < 256 || (piece > 256 && 2 * planes * rows * piece > kPieceBytes)) std::printf("piece %ld %ld %d\\n", (long)n, (long)c, parts);
+                if (piece >= c + 256) std::printf("room %ld %ld %d\\n", (long)n, (long)c, parts);
+                for (int64_t d = 1; d <= (1 << 20); d = d * 9 + 5) {
+                    const int64_t each = da_split(n, d, piece, parts), splits = ceil_div(piece, each);
+                    const TileSize da = tile_for_da(n, d);
+                    const int64_t tiles = tiles_of(d, n, dims_of(da, parts, true));
+                    if (each % 32 || (splits > 1 && (each < 128 || tiles * splits > (da == kTileLarge ? 256 : 512)))) std::printf("split %ld %ld %ld %d\\n", (long)n, (long)c, (long)d, parts);
+                }
+            }
+    """)
+    assert out == "", out[:2000]
