@@ -822,24 +822,32 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
     float2 *const sums = reinterpret_cast<float2 *>(ws + s.sums);
     float *const hits = reinterpret_cast<float *>(ws + s.hits), *const lse = reinterpret_cast<float *>(ws + s.lse);
     const int tiles_x = static_cast<int>(s.tiles_x), tiles_y = static_cast<int>(s.tiles_y);
-// (float32 has no half tiles: the kernel of its middle ones stands there)
-#define DQ_HALF(kernel, what) kernel<what, kInParts ? 128 : 256, kInParts ? 64 : 128, 2, 2, 1, kInParts ? 2 : 3, kP>
-#define DQ_GRID(threads) grid, threads, 0, st
     constexpr bool kInParts = TYPE == DQ_F32;
-    constexpr int kH = kInParts ? 1 : 2, kP = kInParts ? 3 : 1;
     dim3 grid(static_cast<unsigned>(tiles_x * tiles_y));
     // gradients: kept of the first piece
     const bool products = q.grad && (q.da || q.dw);
     const int64_t plane = s.rows_g * s.ldg;
     u16 *const g = reinterpret_cast<u16 *>(ws + s.g);
     const Kept kept = products ? Kept{g, s.ldg, plane, std::min(s.piece, c), reinterpret_cast<float *>(ws + s.target_z)} : Kept{};
+    // (Rows that end inside of a step: the smaller tiles' stages are two steps, and look in any case.  float32 has no half tiles.)
     constexpr int kEdged = kInParts ? TYPE : TYPE | kEdge;
     const bool edge = (s.direct_a || s.direct_w) && s.d % 32;
-    if (edge) DQ_TILE_CASE(scores_kernel, kEdged, kInParts, s.tile, (DQ_HALF(scores_kernel, kEdged)), (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept)
-    else DQ_TILE_CASE(scores_kernel, TYPE, kInParts, s.tile, (DQ_HALF(scores_kernel, TYPE)), (scores_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept)
+#define DQ_EDGE(kernel, size, ...) edge ? DQ_TILE_LAUNCH(kernel, kEdged, size, __VA_ARGS__) : DQ_TILE_LAUNCH(kernel, TYPE, size, __VA_ARGS__)
+#define DQ_SCORES w, a, kd, n, c, 1.0f / tau, targets, tiles_x, tiles_y, sums, hits, kept
+    switch (s.tile) {
+    case kTileLarge: DQ_EDGE(scores_kernel, Large, DQ_SCORES); break;
+    case kTileHalf:
+        if constexpr (kInParts) return DQ_ERR_UNSUPPORTED;
+        else DQ_EDGE(scores_kernel, Half, DQ_SCORES);
+        break;
+    case kTileMiddle: DQ_EDGE(scores_kernel, Middle, DQ_SCORES); break;
+    case kTileFew: DQ_TILE_LAUNCH(scores_kernel, TYPE, Few, DQ_SCORES); break;
+    case kTileFewest: DQ_TILE_LAUNCH(scores_kernel, TYPE, Fewest, DQ_SCORES); break;
+    }
+#undef DQ_SCORES
     DQ_LAUNCH_CHECK();
     const Finish finish{sums, hits, tiles_x, entropy, tau * tau, q.loss, q.lse, q.status};
-    const bool finish_later = products && s.pieces == 1 && n <= 256 && c <= 4096;      // (by the gradients' first kernel)
+    const bool finish_later = products && s.pieces == 1 && n <= 256 && c <= 4096 && s.td.x < 256;      // (by the gradients' first kernel)
     if (!finish_later) {
         const unsigned blocks = static_cast<unsigned>(finish_blocks(n));
         if (n <= kFinishFew) finish_kernel<1><<<blocks, 256, 0, st>>>(finish, n, targets, q.grad ? lse : nullptr);
@@ -865,38 +873,69 @@ static int32_t class_run(const ClassCall &q, const ClassPlan &s)
         if (at == 0) {
             const int64_t cols = up(have, 32);
             const dim3 spans(static_cast<unsigned>((cols + 2047) / 2048), static_cast<unsigned>(std::min<int64_t>(rows_k, 65535)));
-            const int width = kInParts ? 64 : s.td.x;
-#define DQ_KEPT(XT, LATER) kept_kernel<TYPE, XT, LATER><<<spans, 256, 0, st>>>(kept, cols, rows_k, n, finish, targets, lse, q.weight, weight_max)
-            if (finish_later) width == 64 ? DQ_KEPT(64, true) : width == 128 ? DQ_KEPT(128, true) : DQ_KEPT(256, true);
-            else width == 64 ? DQ_KEPT(64, false) : width == 128 ? DQ_KEPT(128, false) : DQ_KEPT(256, false);
+#define DQ_KEPT(x, later) kept_kernel<TYPE, x, later><<<spans, 256, 0, st>>>(kept, cols, rows_k, n, finish, targets, lse, q.weight, weight_max)
+            if (kept_whole(kInParts, s.td.x)) {
+                finish_later ? DQ_KEPT(64, true) : DQ_KEPT(64, false);
+            } else if constexpr (!kInParts) {
+                if (s.td.x == 256) DQ_KEPT(256, false);          // (too many classes or rows to finish later)
+                else finish_later ? DQ_KEPT(128, true) : DQ_KEPT(128, false);
+            }
 #undef DQ_KEPT
         } else {
             const int tiles_p = static_cast<int>((have + s.td.x - 1) / s.td.x);
             grid = dim3(static_cast<unsigned>(tiles_p * tiles_y));
-            if (edge) DQ_TILE_CASE(grad_kernel, kEdged, kInParts, s.tile, (DQ_HALF(grad_kernel, kEdged)), (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
-                                   q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
-            else DQ_TILE_CASE(grad_kernel, TYPE, kInParts, s.tile, (DQ_HALF(grad_kernel, TYPE)), (grad_kernel<TYPE, 64, 16, 4, 1, kH, 4, kP>), DQ_GRID, w, a, kd, n, c, at, have, 1.0f / tau, targets, lse,
-                              q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane)
+            // (Several pieces are 21 turns of large tiles or more: middle ones, 1.05 times as long at best, are not taken.)
+#define DQ_GRAD w, a, kd, n, c, at, have, 1.0f / tau, targets, lse, q.weight, weight_max, tiles_p, tiles_y, g, s.ldg, plane
+            switch (s.tile) {
+            case kTileLarge: DQ_EDGE(grad_kernel, Large, DQ_GRAD); break;
+            case kTileHalf:
+                if constexpr (kInParts) return DQ_ERR_UNSUPPORTED;
+                else DQ_EDGE(grad_kernel, Half, DQ_GRAD);
+                break;
+            case kTileMiddle: return DQ_ERR_UNSUPPORTED;
+            case kTileFew: DQ_TILE_LAUNCH(grad_kernel, TYPE, Few, DQ_GRAD); break;
+            case kTileFewest: DQ_TILE_LAUNCH(grad_kernel, TYPE, Fewest, DQ_GRAD); break;
+            }
+#undef DQ_GRAD
         }
         DQ_LAUNCH_CHECK();
         if (q.da) {
             const Operand piece{w.p + at * w.ld, w.ld, c - at, w.cols, w.plane};
             const int tx = static_cast<int>((s.d + s.td_da.x - 1) / s.td_da.x), ty = static_cast<int>((n + s.td_da.y - 1) / s.td_da.y);
             grid = dim3(static_cast<unsigned>(tx * ty), static_cast<unsigned>(s.splits));
-            DQ_TILE_CASE(da_kernel, TYPE, kInParts, s.tile_da, (DQ_HALF(da_kernel, TYPE)), (da_kernel<TYPE, 128, 16, 4, 1, kH, 4, kP>), DQ_GRID, piece, go, up(have, 32), s.per_split, n, s.d, tx,
-                         ty, partial, s.dp, at == 0, targets, post, weight_max, da, q.ldda, vector_da)
+#define DQ_DA piece, go, up(have, 32), s.per_split, n, s.d, tx, ty, partial, s.dp, at == 0, targets, post, weight_max, da, q.ldda, vector_da
+            switch (s.tile_da) {
+            case kTileLarge: DQ_TILE_LAUNCH(da_kernel, TYPE, Large, DQ_DA); break;
+            case kTileMiddle: DQ_TILE_LAUNCH(da_kernel, TYPE, Middle, DQ_DA); break;
+            case kTileFew: DQ_TILE_LAUNCH(da_kernel, TYPE, Few, DQ_DA); break;
+            case kTileFewest: DQ_TILE_LAUNCH(da_kernel, TYPE, FewestAcross, DQ_DA); break;
+            case kTileHalf: return DQ_ERR_UNSUPPORTED;           // (never: tile_for_da)
+            }
+#undef DQ_DA
             DQ_LAUNCH_CHECK();
         }
         if (q.dw) {
             const int tx = static_cast<int>((s.d + s.td_dw.x - 1) / s.td_dw.x), ty = static_cast<int>((have + s.td_dw.y - 1) / s.td_dw.y);
             grid = dim3(static_cast<unsigned>(tx * ty));
-            DQ_TILE_CASE(dw_kernel, TYPE, kInParts, s.tile_dw, (DQ_HALF(dw_kernel, TYPE)), (dw_kernel<TYPE, 64, 64, 2, 2, kH, 4, kP>), DQ_GRID, az, go, s.rows_z, have, s.d, tx, ty, post, weight_max,
-                         static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw)
+#define DQ_DW az, go, s.rows_z, have, s.d, tx, ty, post, weight_max, static_cast<Mem *>(q.dw) + at * q.lddw, q.lddw
+            switch (s.tile_dw) {                                 // (half ones are through before large ones wherever there are any)
+            case kTileLarge:
+                if constexpr (kInParts) DQ_TILE_LAUNCH(dw_kernel, TYPE, Large, DQ_DW);
+                else return DQ_ERR_UNSUPPORTED;
+                break;
+            case kTileHalf:
+                if constexpr (kInParts) return DQ_ERR_UNSUPPORTED;
+                else DQ_TILE_LAUNCH(dw_kernel, TYPE, Half, DQ_DW);
+                break;
+            case kTileMiddle: DQ_TILE_LAUNCH(dw_kernel, TYPE, Middle, DQ_DW); break;
+            case kTileFew: DQ_TILE_LAUNCH(dw_kernel, TYPE, Few, DQ_DW); break;
+            case kTileFewest: return DQ_ERR_UNSUPPORTED;         // (never: tile_for_dw)
+            }
+#undef DQ_DW
             DQ_LAUNCH_CHECK();
         }
     }
-#undef DQ_GRID
-#undef DQ_HALF
+#undef DQ_EDGE
     if (q.da && partial) {
         const int64_t blocks = std::min<int64_t>((n * ((s.d + 3) / 4) + 255) / 256, 1 << 16);
         da_finish_kernel<TYPE><<<static_cast<unsigned>(blocks), 256, 0, st>>>(partial, static_cast<int>(s.splits), n, s.d, s.dp, targets, post, weight_max, da,

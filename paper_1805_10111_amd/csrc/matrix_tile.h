@@ -35,7 +35,6 @@ typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 
 constexpr int kStepBytes = 64;                 // of k in a product of the matrix cores, per row of an operand stored along k
 constexpr int kStepRows = 32;                  // of k, for an operand stored across it (16-bit numbers)
-constexpr int kRing = 4;                       // stages in LDS, of H steps each
 
 // An operand in memory.  Its row i (row k where it is stored across k) begins at p + i * ld bytes; rows is how many there are.
 // Nothing outside of it matters: rows past the last are zeros, and k past its end.
@@ -657,15 +656,15 @@ __device__ __forceinline__ void tile_of_block(int block, int tiles_x, int tiles_
     tx = in / high;
 }
 
-// kernel<what, x, y, WX, WY, H, R, P> in a tile's size: its wavefronts, steps a stage, stages in the ring, parts of a number.  half, few: the
-// kernels of half tiles and of the smallest.
-#define DQ_TILE_CASE(kernel, what, parts, size, half, few, launch, ...)                                                        \
-    switch (size) {                                                                                                            \
-    case kTileLarge: kernel<what, 256, parts ? 128 : 256, 2, 4, 1, parts ? 2 : 4, parts ? 3 : 1><<<launch(threads_of(kTileLarge))>>>(__VA_ARGS__); break;     \
-    case kTileHalf: half<<<launch(threads_of(kTileHalf))>>>(__VA_ARGS__); break;                                                                 \
-    case kTileMiddle: kernel<what, 128, parts ? 64 : 128, 2, 2, 1, parts ? 2 : 4, parts ? 3 : 1><<<launch(threads_of(kTileMiddle))>>>(__VA_ARGS__); break;     \
-    case kTileFew: kernel<what, 64, 64, 2, 2, parts ? 1 : 2, 4, parts ? 3 : 1><<<launch(threads_of(kTileFew))>>>(__VA_ARGS__); break;          \
-    case kTileFewest: few<<<launch(threads_of(kTileFewest))>>>(__VA_ARGS__); break;                                                                \
-    }
+// The launch of a kernel in a tile's size: `what`, then x, y, the wavefronts that share them, steps a stage, stages in the ring, parts of a number
+// (kInParts: float32's three).  The callers list the sizes that their rules give.
+#define DQ_TILE_Large(parts) 256, parts ? 128 : 256, 2, 4, 1, parts ? 2 : 4, parts ? 3 : 1
+#define DQ_TILE_Half(parts) 256, 128, 2, 2, 1, 3, 1
+#define DQ_TILE_Middle(parts) 128, parts ? 64 : 128, 2, 2, 1, parts ? 2 : 4, parts ? 3 : 1
+#define DQ_TILE_Few(parts) 64, 64, 2, 2, parts ? 1 : 2, 4, parts ? 3 : 1
+#define DQ_TILE_Fewest(parts) 64, 16, 4, 1, parts ? 1 : 2, 4, parts ? 3 : 1
+#define DQ_TILE_FewestAcross(parts) 128, 16, 4, 1, parts ? 1 : 2, 4, parts ? 3 : 1
+constexpr TileSize kTileFewestAcross = kTileFewest;
+#define DQ_TILE_LAUNCH(kernel, what, size, ...) kernel<what, DQ_TILE_##size(kInParts)><<<grid, threads_of(kTile##size), 0, st>>>(__VA_ARGS__)
 
 }  // namespace dq

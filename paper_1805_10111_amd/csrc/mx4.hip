@@ -231,10 +231,17 @@ static int32_t product4(const dq_mx4 &a, const dq_mx4 &w, void *out, int64_t ld,
     const TileDims t = dims_of(size, false, false);
     const int64_t tiles_x = (w.n + t.x - 1) / t.x, tiles_y = (a.n + t.y - 1) / t.y;
     auto operand = [](const dq_mx4 &q) { return Operand{reinterpret_cast<const char *>(q.codes), q.ld_codes, q.n, static_cast<int32_t>(groups_of(q.d) * 32), 0, q.scales, q.ld_scales}; };
-#define DQ_GRID(threads) static_cast<unsigned>(tiles_x * tiles_y), threads, 0, st
-    DQ_TILE_CASE(mx4_product_kernel, TYPE, false, size, (mx4_product_kernel<TYPE, 128, 128, 2, 2, 1, 4, 1>), (mx4_product_kernel<TYPE, 64, 16, 4, 1, 2, 4, 1>), DQ_GRID, operand(w), operand(a), groups_of(a.d) * 32,
-                 static_cast<int>(tiles_x), static_cast<int>(tiles_y), static_cast<typename Num<TYPE>::Mem *>(out), ld)
-#undef DQ_GRID
+    constexpr bool kInParts = false;
+    const unsigned grid = static_cast<unsigned>(tiles_x * tiles_y);
+#define DQ_PRODUCT operand(w), operand(a), groups_of(a.d) * 32, static_cast<int>(tiles_x), static_cast<int>(tiles_y), static_cast<typename Num<TYPE>::Mem *>(out), ld
+    switch (size) {
+    case kTileLarge: DQ_TILE_LAUNCH(mx4_product_kernel, TYPE, Large, DQ_PRODUCT); break;
+    case kTileMiddle: DQ_TILE_LAUNCH(mx4_product_kernel, TYPE, Middle, DQ_PRODUCT); break;
+    case kTileFew: DQ_TILE_LAUNCH(mx4_product_kernel, TYPE, Few, DQ_PRODUCT); break;
+    case kTileFewest: DQ_TILE_LAUNCH(mx4_product_kernel, TYPE, Fewest, DQ_PRODUCT); break;
+    case kTileHalf: return DQ_ERR_UNSUPPORTED;                   // (not asked for)
+    }
+#undef DQ_PRODUCT
     DQ_LAUNCH_CHECK();
     return DQ_OK;
 }

@@ -184,3 +184,33 @@ def test_pieces_and_splits_of_many_classes(tmp_path):
             }
     """)
     assert out == "", out[:2000]
+
+
+def test_sizes_that_the_rules_for_tiles_never_give(tmp_path):
+    """The kernels that exist: no half tiles for da, no large ones for dW of 16-bit numbers, none of 16 rows for dW, no middle ones for scores that
+    are multiplied again, none 256 wide where a row's sums are left to the gradients (at most 256 rows of 4096 classes)."""
+    out = _sweep(tmp_path, """
+    long several = 0;
+    for (int64_t n = 1; n < (1ll << 28); n += 1 + n / 23)
+        for (int parts = 0; parts < 2; ++parts) {
+            for (int64_t c = 1; c < (1ll << 30); c += 1 + c / 97) {
+                const TileSize s = tile_for_rows(c, n, parts, true);
+                const TileDims t = dims_of(s, parts, false);
+                if (parts && s == kTileHalf) std::printf("half %ld %ld\\n", (long)n, (long)c);
+                const int64_t piece = piece_of(c, ceil_div(n, t.y) * t.y, planes_of_g(parts, t.x));
+                several += c > piece;
+                if (c > piece && s == kTileMiddle) std::printf("middle %ld %ld %d\\n", (long)n, (long)c, parts);
+                for (int64_t d = 1; d <= (1 << 20); d = d * 5 + 3) {
+                    const TileSize dw = tile_for_dw(n, c, d, piece, parts);
+                    if (dw == kTileFewest || dw == (parts ? kTileHalf : kTileLarge)) std::printf("dw %ld %ld %ld %d\\n", (long)n, (long)c, (long)d, parts);
+                }
+            }
+            for (int64_t d = 1; d <= (1 << 20); d += 1 + d / 11)
+                if (tile_for_da(n, d) == kTileHalf) std::printf("da %ld %ld\\n", (long)n, (long)d);
+        }
+    for (int64_t n = 1; n <= 256; ++n)
+        for (int64_t c = 1; c <= 4096; ++c)
+            if (dims_of(tile_for_rows(c, n, false, true), false, false).x > 128) std::printf("wide %ld %ld\\n", (long)n, (long)c);
+    if (several < 1000) std::printf("few of several pieces: %ld\\n", several);
+    """)
+    assert out == "", out[:2000]
