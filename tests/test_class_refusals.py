@@ -178,3 +178,13 @@ def test_products_in_four_bits_that_no_launch_takes(n):
     w, a = mx4(n=1 << 30, d=128, ld_codes=64, ld_scales=4), mx4(n=n, d=128, ld_codes=64, ld_scales=4)
     assert api._lib.dq_mx4_product(C.byref(a), C.byref(w), AT, BF16, 1 << 30, None) == dq.ERR_UNSUPPORTED
     assert scores(w, n=n, ld=1 << 30) == dq.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("t,planes,wide", [(F32, 3, 256), (F16, 1, 256), (BF16, 1, 256)])
+def test_the_workspace_holds_one_piece_of_gradients(t, planes, wide):
+    """8192 rows of a million classes: 1 GB of g, three sums a tile and row, packed operands; and what is small beside these (da's partial sums,
+    one value a row: below 128 MB)."""
+    n, c, d = 8192, 1 << 20, 256
+    known = 12 * n * (c // wide) + 2 * planes * n * d + (2 * planes * (n + c) * d if t == F32 else 0)
+    piece = size(problem(t, n, c, d, lda=d, ldw=d)) - known
+    assert (1 << 30) - 2 * planes * n * 256 <= piece <= (1 << 30) + (128 << 20)
