@@ -318,7 +318,8 @@ int32_t dq_acc_snapshot(const float *xsum, int64_t m, int64_t d, float *x_snap_o
  * Types of the features and of the model (one for both, and for their gradients): float32, float16, bfloat16.  Sums, scores, their
  * maxima and sums of exponentials, and losses are float32 (what 16-bit gradients are made from: at dq_class_grad); products of
  * float32 are carried out to float32's own precision on the matrix cores, in three bfloat16 parts (magnitudes of 2^127 * 1.99 and
- * more count as infinite; anything not finite gives losses that are not finite). */
+ * more count as infinite; of those below 2^-110 what is left are multiples of 2^-133; anything not finite gives losses that are not
+ * finite). */
 #define DQ_F32   0
 #define DQ_F16   1
 #define DQ_BF16  2
@@ -373,7 +374,7 @@ int32_t dq_class_grad(const dq_classes *prob /*host*/, const int32_t *label, con
 /* Distillation: with q_t = softmax(logit_t / tau) over the entries of row t and p_t = softmax(z_t / tau) over all classes,
  *   loss_out[t] = tau^2 sum_j q_tj (log q_tj - log p_tj),   lse_out[t] = log sum_j exp(z_tj / tau).
  * A row without an entry (or whose logits are all -inf) is left out, as above.  Entries with a class of c or more are not there, and
- * set status bit 1.  An entry whose logit is a NaN or +inf makes its row's loss and gradients NaN (status bit 0). */
+ * set status bit 1.  An entry whose logit is a NaN or +inf makes its row's loss and da, and dW of its classes, NaN (status bit 0). */
 int32_t dq_distill_loss(const dq_classes *prob /*host*/, const dq_teacher *teacher /*host*/, float *loss_out, float *lse_out,
                         uint32_t *status, void *ws, int64_t ws_bytes, void *stream);
 /* The same with gradients:  g_tj = scale weight_t tau (p_tj - q_tj). */

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(1024) void weight_max_kernel(const float *__restric
 
 // One block of 64 threads per row: q = softmax(logit / tau) over the entries, sorted by class (bitonic, in LDS).
 // entropy[t] = sum q log q.  Rows without an entry: all classes kNoClass.  (Differences are scaled, not logits: entries of the type's lowest
-// value stay finite at any temperature.)  4096 rows of 64 entries: 12 us.
+// value stay finite at any temperature.)  4096 rows of 64 entries: 12 to 14 us.
 constexpr int kTeacherThreads = 64;
 __global__ __launch_bounds__(kTeacherThreads) void teacher_kernel(const int32_t *__restrict__ cls_in, const float *__restrict__ logit, int64_t ld,
                                                                   int k, int pow2, int64_t c, float inv_tau, int32_t *__restrict__ cls,
@@ -236,8 +236,8 @@ struct KeptUnit {
 };
 
 // The sums of a tile's row: its maximum, the sum of exp above it, the targets' sum q z; [tile][row].
-// Bound by the matrix cores where there are many rows (8192 x 47236 x 4096 in bfloat16 2.67 ms, 1190 TFLOP/s, a fifth of it the tiles'
-// ends; 2048 x 20958 x 1000 105 us), by the model's bytes where there are few (1 x 47236 x 4096 80 us, 4.8 TB/s).
+// Bound by the matrix cores where there are many rows (8192 x 47236 x 4096 in bfloat16 2.67 to 2.84 ms on different cards, 1120 to 1190 TFLOP/s,
+// a fifth of it the tiles' ends; 2048 x 20958 x 1000 105 to 109 us), by the model's bytes where there are few (1 x 47236 x 4096 80 us, 4.8 TB/s).
 template <int WHAT, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave, 2) void scores_kernel(Operand w, Operand a, int64_t k, int64_t n, int64_t c, float inv_tau, Targets targets,
                                                                int tiles_x, int tiles_y, float2 *__restrict__ sums, float *__restrict__ hits, Kept kept)
@@ -602,7 +602,7 @@ __device__ __forceinline__ float gradient_unit(int type, float post, const float
     return type == DQ_F16 ? post * ((weight_max ? weight_max[0] : 1.0f) / kF16Unit) : post;
 }
 
-// (Matrix cores: 8192 x 47236 x 4096 in bfloat16 2.16 ms, 1470 TFLOP/s.)
+// (Matrix cores: 8192 x 47236 x 4096 in bfloat16 2.15 to 2.20 ms, 1440 to 1475 TFLOP/s.)
 // da of a piece, one split of its classes per blockIdx.y: partial sums [split][n][ldp] in float32, added to what the pieces before left.
 // Where one launch has it all (partial null) da itself.
 template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
@@ -660,7 +660,8 @@ __global__ __launch_bounds__(256) void da_finish_kernel(const float *__restrict_
 }
 
 // dw of a piece.  Both operands are stored across k: no LDS bank is met twice, and half tiles, two blocks to a compute unit, are the
-// faster ones (8192 x 47236 x 4096 in bfloat16 2.33 ms, 1360 TFLOP/s; 256 x 256 2.46).
+// faster ones (8192 x 47236 x 4096 in bfloat16 2.29, 256 x 256 2.46 ms; on other cards 2.33 to 2.50, 1270 to 1360 TFLOP/s).  16-bit half tiles need two
+// registers more than there are and keep them in scratch memory (12 bytes a lane).
 template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave, 2) void dw_kernel(Operand a, Operand g, int64_t k, int64_t piece, int64_t d, int tiles_x, int tiles_y,
                                                            float post, const float *__restrict__ weight_max,

@@ -14,7 +14,7 @@
 // What bounds it: the matrix cores.  256 x 256 with eight wavefronts (a wavefront multiplies 128 x 64: 12 reads of LDS for 32
 // products) needs 96 KB of LDS reads per 1024 cycles of matrix-core work, which LDS does in 400, and each byte of memory is used for
 // 256 products.  A step takes 1.3 times the 1024 cycles; at 1.7 to 1.8 GHz, which is what the clocks are held to under this
-// load, that is 1470 TFLOP/s in bfloat16 (n = 8192 rows of 47236 classes times 4096 columns, where a tile is 1476 steps).
+// load, that is 1440 to 1475 TFLOP/s in bfloat16 (n = 8192 rows of 47236 classes times 4096 columns, where a tile is 1476 steps).
 #pragma once
 
 #include <hip/hip_bf16.h>
@@ -392,7 +392,7 @@ struct TileProduct {
     // Stores the tile row by row j, value(m, n) the four results of subtile (m, n) in memory's type: out: where the tile's first row
     // begins, rows, cols: how many of the tile's rows and of their columns there are.  A lane's four results are 8 or 16 bytes of one of sixteen
     // rows; each wavefront turns them, through its part of LDS, into up to 256 neighbouring bytes of a row.  (The
-    // gradient of a 20011 x 1001 float16 model: written four numbers at a time 83 us, so 50.)
+    // gradient of a 20011 x 1001 float16 model, on 256 x 256 tiles: written four numbers at a time 83 us, so 50.)
     template <class Mem, class Value>
     __device__ __forceinline__ void store(Mem *out, int64_t ld, int64_t rows, int64_t cols, Value value) const
     {

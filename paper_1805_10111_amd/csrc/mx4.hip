@@ -71,8 +71,9 @@ __device__ __forceinline__ Place place_of(uint32_t i, uint32_t per, int64_t row0
     return Place{row0 + r, i - r * per};
 }
 
-// A thread takes eight numbers: 16 or 32 bytes read, 4 written; four neighbouring lanes share a block.  What bounds it is memory:
-// 47236 x 4096 in bfloat16 (490 MB) 94 us, in float32 (877 MB) 154 us; two and four items a thread 90 to 95 and 97 to 100, 160 and 169.
+// A thread takes eight numbers: 16 or 32 bytes read, 4 written; four neighbouring lanes share a block.  What bounds it is memory: 47236 x 4096
+// in bfloat16 (490 MB) 94 to 108 us on different cards, in float32 (877 MB) 154.  (Two and four items a thread, where one took 94 and 154: 90 to 95 and
+// 97 to 100, 160 and 169.)
 template <int TYPE>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const typename Num<TYPE>::Mem *__restrict__ v, int64_t n, int64_t rows, uint32_t d, int64_t ld,
                                                            uint8_t *__restrict__ codes, int64_t ld_codes, uint8_t *__restrict__ scales,
@@ -113,8 +114,8 @@ __device__ __forceinline__ void store_eight(typename Num<TYPE>::Mem *to, const f
     }
 }
 
-// The inverse, AT_ONCE items a thread requested together.  47236 x 4096 to bfloat16 (490 MB): one 107 us, two 98, four 88; to float32
-// (877 MB) 172, 220 and 228: there the stores are twice as long, and one it is.
+// The inverse, AT_ONCE items a thread requested together.  47236 x 4096 to bfloat16 (490 MB): one 107 us, two 98, four 88 (73 right behind the
+// quantizer, whose codes are in the cache yet); to float32 (877 MB) 166 to 172, 220 and 228: there the stores are twice as long, and one it is.
 template <int TYPE, int AT_ONCE>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes, int64_t ld_codes, const uint8_t *__restrict__ scales,
                                                              int64_t ld_scales, int64_t n, int64_t rows, uint32_t d, typename Num<TYPE>::Mem *__restrict__ out,
@@ -147,9 +148,9 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__re
     }
 }
 
-// Few rows: bound by w's codes (1 x 47236 x 4096, 103 MB, 17.7 us).  Many: 8192 x 47236 x 4096 980 us, 3230 TFLOP/s: a step is as many
-// bytes of LDS as 16-bit numbers take, with the scales to bring there, for as many cycles of the matrix cores, and takes twice these;
-// 200 us are the results' (774 MB in bfloat16).
+// Few rows: bound by w's codes (1 x 47236 x 4096, 103 MB, 18 us).  Many: 8192 x 47236 x 4096 0.98 to 1.05 ms on different cards, 3020 to 3230
+// TFLOP/s, the matrix cores busy 38 % of the time: a step is as many bytes of LDS, and as many cycles of the matrix cores, as in 16 bits, with the
+// scales to bring there besides, and takes twice these cycles; a tile is only 32 steps; 200 us are the results' (774 MB in bfloat16).
 template <int TYPE, int XT, int YT, int WX, int WY, int H, int R, int P>
 __global__ __launch_bounds__(WX *WY *kWave) void mx4_product_kernel(Operand w, Operand a, int64_t k, int tiles_x, int tiles_y,
                                                                     typename Num<TYPE>::Mem *__restrict__ out, int64_t ld)
