@@ -360,13 +360,10 @@ inline GramPlan gram_plan(int64_t side, int64_t k, int products, int jobs)
 }
 // Whether two products go together, in one launch: where one leaves most of the chip idle.
 inline bool gram_together(const GramPlan &p) { return static_cast<int64_t>(p.tiles) * p.splits <= (p.size == kTileLarge ? 64 : 256); }
-// Whether 16-bit updates of `side` by `deep` go through the small matrices: twelve or so products of side^2 deep against two and a half, and 26 of side^3 (float16
-// step by step: 23 and 8 of side^3) at 1000 TFLOP/s, and the launches, 17 and 26 of some 4 us.
-inline bool small_matrices(int64_t side, int64_t deep, bool f16)
-{
-    const double s = static_cast<double>(side), l = static_cast<double>(deep), unit = 2.0 * s * s / 1e9;
-    return unit * (2.5 * l + 25.5 * s) + 26 * 4 < unit * ((f16 ? 22.5 : 11.5) * l + (f16 ? 7.5 : 2.5) * s) + 17 * 4 || f16;
-}
+// Whether 16-bit updates of `side` by `deep` go through the small matrices: float16 always, bfloat16 where that is faster than step by step (about 2.5 side^2 deep and
+// 32 side^3 against 20 and 9): us for five steps of 1000 x 1000 299 and 262, x 1250 312 and 325, x 2000 319 and 392; 2500 x 3000 1581 and 1535; 4096 x 4096
+// 4917 and 3977, x 5000 5099 and 5425, x 8192 5245 and 6731; 100 x 4000 125 and 161.  (Small ones near the border are 5 us, of 150 to 220, off it either way.)
+inline bool small_matrices(int64_t side, int64_t deep, bool f16) { return f16 || 5 * deep > 6 * side; }
 // Tiles of X's next value, rows x cols numbers.
 inline TileSize update_tile(int64_t cols, int64_t rows)
 {

@@ -6,16 +6,16 @@
 //
 // Two ways.  Step by step, as the formulas say: products of s^2 l (s the shorter side, l the longer) two or three times a step.  Or, 16-bit types, through the small
 // matrices alone: with Q = a + B, A of the next step is Q A Q, and X after all steps is P X, P the product of the Q: s^2 l once for A, twice (P in two parts) for P X, and
-// four products of s^3 a step, which is less where l is more than 2.6 s (float16: more exact, and less anywhere).  P is held less a^steps times one, and Q less a:
+// four products of s^3 a step, which is less where l is more than 1.2 s (float16 goes that way always).  P is held less a^steps times one, and Q less a:
 // what is held then is as small as A is where a matrix has nothing.
 //
 // What is rounded to what.  An error E of A or Q acts as (1 + E) X, which turns and stretches what is there by E; an error added to X puts
-// something where a matrix of low rank has nothing, and every later step makes that 3.4445 times as large, 485 times in five.  So step by step X is the
-// sum of two float16 (22 bits), whatever A and B = b A + c A^2 are: for bfloat16 one float16 (A made from X's upper one), results 10^-4 to
-// 1.4 10^-3 off in norm before they are rounded, whatever the rank; for float16 and float32 two.  (X in one float16: 0.001 off where all singular values
-// count, 0.1 for one direction; in one bfloat16 0.012 and 0.75.)  Through the small matrices X is the matrix that was given, exactly, and A, B and P are two
-// float16 each: 10^-5 (singular values of one size) to 6 10^-4 (one far beyond the others).  X, A, B and P are held times 2^14, 2^14, 2^12 (through the small
-// matrices 2^13) and 2^6, so that entries of a matrix of 2^28 numbers are normal float16 ones and P's of five steps (up to 485) in range.
+// something where a matrix of low rank has nothing, and every later step makes that 3.4445 times as large, 485 times in five.  So everything is the sum of two float16, 22
+// bits: X, A and B = b A + c A^2.  (X in one float16: 0.001 off where all singular values count, 0.1 for one direction; in one bfloat16 0.012 and 0.75.  A and B in one,
+// 11 bits: roundings that go either way leave 0.0012 in norm, but those of a matrix whose numbers share their significands are all the same and left 0.006, more than
+// bfloat16's own half step; five steps of 4096 x 4096 took 2.4 ms so, and 4.0 in two.)  Through the small matrices X is the matrix that was given, exactly, and A, B and P
+// are two float16 each: 10^-5 (singular values of one size) to 8 10^-4 (one direction: P X adds up 485 times its result in float32).  X, A, B and P are held times 2^14,
+// 2^14, 2^12 (through the small matrices 2^13) and 2^6, so that entries of a matrix of 2^28 numbers are normal float16 ones and P's of five steps (up to 485) in range.
 //
 // float32 goes step by step: two float16, and three products of their four, are at worst four times float32's rounding, but the sums' and the steps' own
 // roundings are the larger part, 2 10^-6 to 10^-4 in norm as in float32 throughout (256 x 1000 of noise 2.2 and 2.1 10^-6, of rank 1 1.26 and 1.21 10^-4; three
@@ -121,9 +121,6 @@ __global__ __launch_bounds__(256) void orthogonal_pack_kernel(const typename Num
     }
 }
 
-// Step by step: parts of A and B (X has two).
-template <int TYPE>
-constexpr int kPartsOfA = TYPE == DQ_BF16 ? 1 : 2;
 constexpr float kUpQ = 8192.0f, kUpP = 64.0f;                       // through the small matrices
 constexpr int kStepsOfP = 5;
 
@@ -435,9 +432,8 @@ static OrthogonalPlan plan_of(int64_t n, int64_t d)
     p.x_bytes = ceil_div(2 * 2 * p.x_next, 16) * 16;
     p.a_ld = apart(p.side);
     p.a_next = p.side * p.a_ld;
-    p.a_bytes = (p.small ? 2 : kPartsOfA<TYPE>) * 2 * p.a_next;
+    p.a_bytes = 2 * 2 * p.a_next;
     p.matrices = p.small ? 6 : 2;
-    constexpr int kOfA = kPartsOfA<TYPE>;
     const int64_t k = p.tall ? p.rows : p.cols;
     int64_t floats = 0;
     auto plan = [&](int64_t deep, int products, int jobs) {
@@ -445,12 +441,10 @@ static OrthogonalPlan plan_of(int64_t n, int64_t d)
         if (!g.at_once) floats = std::max(floats, g.floats() * jobs);
         return g;
     };
-    p.gram = plan(k, part_products(kOfA, kOfA), 1);
-    p.square = plan(p.side, p.small ? 3 : part_products(kOfA, kOfA), 1);
-    if (p.small) {
-        p.first = plan(k, 1, 1);
-        p.pair = plan(p.side, 3, 2);
-    }
+    p.gram = plan(k, 3, 1);
+    if (TYPE != DQ_F32) p.first = plan(k, 1, 1);
+    p.square = plan(p.side, 3, 1);
+    if (p.small) p.pair = plan(p.side, 3, 2);
     p.sums_bytes = 4 * floats;
     return p;
 }
@@ -505,7 +499,6 @@ template <int TYPE, bool TALL>
 static int32_t orthogonalize(const OrthogonalPlan &p, const void *v, int64_t n, int64_t d, int64_t ld, int32_t steps, void *out, int64_t ldo, uint32_t *status, char *ws, hipStream_t st)
 {
     typedef typename Num<TYPE>::Mem Mem;
-    constexpr int kOfA = kPartsOfA<TYPE>;
     OrthogonalHead *const head = reinterpret_cast<OrthogonalHead *>(ws);
     char *at = ws + sizeof(OrthogonalHead);
     auto take = [&](int64_t bytes, int64_t ld_, int64_t next) {
@@ -565,17 +558,20 @@ static int32_t orthogonalize(const OrthogonalPlan &p, const void *v, int64_t n, 
         const OrthogonalHead *const first = TYPE != DQ_F32 && step == 0 ? head : nullptr;
         void *const last = step + 1 == steps ? out : nullptr;
         const GramJob of_x{whole(now), whole(now), first, kUpA / (kUpX * kUpX), 0.0f, 0.0f, Parts{}, Parts{}, a};
-        if (const int32_t e = gram<kOfA, kOfA, (TALL ? kAcross : kAlong)>(p, p.gram, k, sums, GramJobs{{of_x, of_x}}, 1, st)) return e;
         const GramJob square{small(a), small(a), nullptr, kC * kUpB / (kUpA * kUpA), kB * kUpB / kUpA, 0.0f, a, Parts{}, b};
-        if (const int32_t e = gram<kOfA, kOfA, kMixed>(p, p.square, p.side, sums, GramJobs{{square, square}}, 1, st)) return e;
-        int32_t e;
-        if constexpr (TYPE == DQ_BF16) {                            // the first X is exact in one part
-            e = step == 0 ? update<TYPE, TALL, 1, 1>(p, now, b, 1, kA, 1.0f / kUpB, next, first, last, ldo, n, d, st)
-                          : update<TYPE, TALL, 2, 1>(p, now, b, 2, kA, 1.0f / kUpB, next, first, last, ldo, n, d, st);
-        } else {
-            e = update<TYPE, TALL, 2, kOfA>(p, now, b, 2, kA, 1.0f / kUpB, next, first, last, ldo, n, d, st);
+        auto one_step = [&](auto parts, const GramPlan &plan) -> int32_t {          // parts of X
+            constexpr int kOfX = decltype(parts)::value;
+            if (const int32_t e = gram<kOfX, 2, (TALL ? kAcross : kAlong)>(p, plan, k, sums, GramJobs{{of_x, of_x}}, 1, st)) return e;
+            if (const int32_t e = gram<2, 2, kMixed>(p, p.square, p.side, sums, GramJobs{{square, square}}, 1, st)) return e;
+            return update<TYPE, TALL, kOfX, 2>(p, now, b, kOfX, kA, 1.0f / kUpB, next, first, last, ldo, n, d, st);
+        };
+        if constexpr (TYPE == DQ_BF16) {
+            if (step == 0) {                                        // what was given is exact in one
+                if (const int32_t e = one_step(std::integral_constant<int, 1>(), p.first)) return e;
+                continue;
+            }
         }
-        if (e) return e;
+        if (const int32_t e = one_step(std::integral_constant<int, 2>(), p.gram)) return e;
     }
     return DQ_OK;
 }
