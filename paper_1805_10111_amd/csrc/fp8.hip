@@ -290,8 +290,9 @@ __global__ __launch_bounds__(256) void fp8_sum_kernel(const float *__restrict__ 
     }
 }
 
-// Many rows, results of 16 bits: the codes as they are.  8192 x 8192 x 8192 414 us, 2660 TFLOP/s; 8192 x 47236 x 4096 1.27 to 1.45 ms with numbers of different
-// kinds (which draw different power), of which what is stored takes 0.13.
+// Many rows, results of 16 bits: the codes as they are.  How long it takes goes by the numbers, which draw different power: 8192 x 8192 x 8192, the same product
+// again and again, 412 us (2670 TFLOP/s) of normally distributed numbers, 374 of whole ones from -2 to 2, 335 of ones; 8192 x 47236 x 4096 1297, 1201 and 1095 us, of which
+// what is stored is some 130 (a pass on new rows into another result, their quantization of 20 us included: 1500).
 template <int TYPE, int XT, int YT, int WX, int WY, int R>
 __global__ __launch_bounds__(WX *WY *kWave) void fp8_tile_kernel(dq_fp8 w, dq_fp8 a, int per_split, int tiles_x, int tiles_y, typename Num<TYPE>::Mem *__restrict__ out, int64_t ld,
                                                                  float *__restrict__ sums)

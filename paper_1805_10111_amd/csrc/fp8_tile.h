@@ -5,8 +5,8 @@
 // the others) those whose rows begin at the same banks then read different chunks.  A lane holds chunks 2 h and 2 h + 1 of either half of row lane % 32, h = lane / 32,
 // and of a result the four neighbouring i at 8 q + 4 h, q = 0 .. 3, of column j = lane % 32.
 // Rings of two where the matrix cores bound, for one large tile or two middle ones to a compute unit; four where there is one middle tile to a unit, for a stage there
-// takes as long as its loads, divided by those under way.  (Stages of half a block in rings of four, whose loads are of half a line of the cache: 8192 x 47236 x 4096
-// 1497 us, whole blocks in a ring of two 1420; middle tiles, 5003 x 1001 x 2049, 25 and 20.)
+// takes as long as its loads, divided by those under way.  (Stages of half a block in rings of four, whose loads are of half a line of the cache, took 5%
+// longer at 8192 x 47236 x 4096 and 8% at 8192 x 8192 x 8192; middle tiles, 5003 x 1001 x 2049, 25 us, whole blocks 20.)
 //
 // The scales of two blocks are brought at a time, by the thread whose row they are of, a turn of the ring ahead, and lie in LDS as [row % 32][row / 32], so
 // that a lane reads those of all its subtiles at once.
@@ -246,7 +246,7 @@ struct Fp8Tile {
 
     // Stores the tile row by row j (16 bits a number): each wavefront turns 32 rows of all its columns at a time, through its part of the first two stages, into
     // as many neighbouring bytes a row as it has (256 of a large tile), which go past the cache.  8192 x 47236 x 4096, whose rows begin anywhere: 128 bytes at a time
-    // 1592 us, 256 1566, and past the cache 1454 (nothing stored: 1322).
+    // 26 us more, not past the cache 112 more (nothing stored: 132 less).
     template <int TYPE>
     __device__ __forceinline__ void store(typename Num<TYPE>::Mem *out, int64_t ld, int64_t rows, int64_t cols) const
     {

@@ -357,7 +357,9 @@ __global__ __launch_bounds__(256) void norm_grad_sums_kernel(NormArgs p, const t
     to[1] = sum[1];
 }
 // ... then 64 columns of all rows a block, which has dgain's sums of them to itself: two launches as well.  float32, with and without these two: 64 x 20958 14.2 and
-// 20.8 us, 64 x 47236 19.6 and 37.1, 1 x 47236 8.9 and 24.3, 128 x 4096 9.7 and 10.2; 256 x 4096 13.7 and 11.2.
+// 20.8 us, 64 x 47236 19.6 and 37.1, 1 x 47236 8.9 and 24.3, 128 x 4096 9.7 and 10.2; 256 x 4096 13.7 and 11.2.  The border goes by rows alone: beyond it, without calls between
+// the launches, 129 x 256 are 7.7 and 5.3 us, x 4096 8.5 and 7.5, but x 8192 9.3 and 10.9, x 20958 21.8 and 24.6, x 47236 31.9 and 37.2; 192 x 47236 42.6 and 46.5, 256 x 20958 34.4 and
+// 33.4.
 template <int TYPE>
 __global__ __launch_bounds__(256) void norm_grad_columns_kernel(NormArgs p, const typename Num<TYPE>::Mem *dy, int64_t lddy, const typename Num<TYPE>::Mem *dh, int64_t lddh,
                                                                 typename Num<TYPE>::Mem *dx, int64_t lddx, const double (*__restrict__ sums)[2], int pieces,
